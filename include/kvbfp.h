@@ -428,6 +428,106 @@ int kvbfp_decode_attention_noalloc(const kvbfp_layout* layout, const kvbfp_cache
                                    const int32_t* perm_k, const int32_t* perm_v, int32_t q_mant_bits,
                                    void* out, void* hip_stream);
 
+/* A rule on the scores of attention over the cache, for kvbfp_decode_attention_scored and kvbfp_accumulate_weights.  Plain data, filled by
+ * the caller; struct_bytes must be sizeof(kvbfp_score_rule); everything else may be zero / NULL.  The last n_q_tokens tokens of a
+ * sequence are the query tokens themselves ("nodes": base = seq_len - n_q_tokens, node j is token base + j; with seq_len < n_q_tokens the
+ * first ones do not exist as keys).  Query token i scores token t as
+ *     y = softmax_scale * q . k                         then, with cap > 0,  y = cap * tanh(y / cap)
+ *     y = y - slopes[query head] * |pos(i) - pos(t)|    with slopes
+ * and sees it if t < seq_len and
+ *     t < prefix_dev[b]   or   ( order(i, t)  and  t >= first_dev[b][i]  and  (window == 0 or pos(i) - pos(t) < window) )
+ *   order : t < base, or node t - base is one that i sees: bit t - base of tree_mask[b][i] (bits of i's ancestors and of i itself in a tree
+ *           of drafted tokens; any mask will do, a node that sees nothing is fine), without tree_mask the nodes up to i itself.
+ *   pos   : t for t < base; for node j base + the number of other nodes that it sees (its depth in the tree; base + j without one).
+ * A query token that sees nothing yields zeros and lse = -infinity.
+ *   cap        : finite, >= 0; 0 = none.
+ *   window     : >= 0; 0 = none.
+ *   slopes     : DEVICE float [n_q_heads] or NULL.
+ *   first_dev  : DEVICE int32 [batch][n_q_tokens] or NULL: the first token of the document that a query token belongs to.
+ *   prefix_dev : DEVICE int32 [batch] or NULL: tokens seen by every query token, whatever else (clamped to [0, seq_len]).
+ *   tree_mask  : DEVICE uint64 [batch][tree_stride], the first n_q_tokens of each row; tree_stride 0 = one tree for all sequences.
+ * Tokens that no query token sees for the window, the documents and the prefix are not read. */
+typedef struct {
+    uint32_t struct_bytes;
+    float cap;
+    int32_t window;
+    int32_t tree_stride;
+    const float* slopes;
+    const int32_t* first_dev;
+    const int32_t* prefix_dev;
+    const uint64_t* tree_mask;
+} kvbfp_score_rule;
+
+/* DEVICE, asynchronous.  Attention for the last n_q_tokens tokens of every sequence with a rule on the scores: kvbfp_decode_attention_multi
+ * (the same products and layouts, 1..64 query tokens that are cached already) with a tree of drafted tokens in place of the causal order,
+ * capped or biased scores, windows, documents, prefixes.  rule = NULL is that call's causal order.
+ *   q, out    : DEVICE [batch][n_q_tokens][n_q_heads][head_dim] of `dtype`, contiguous.
+ *   lse       : DEVICE float [batch][n_q_tokens][n_q_heads] or NULL: the natural logarithm of the sum of exp(y) over the tokens seen.
+ *   workspace : DEVICE, at least kvbfp_scored_workspace_bytes(layout, n_q_heads, n_q_tokens, max_len) bytes, 256-byte aligned.  Calls that may
+ *               run at the same time need one each.
+ * seq_len_dev, max_len, perm_k, perm_v as in kvbfp_decode_attention.  Exponent planes at any address.  n_q_heads * n_q_tokens up to 65535.
+ * Accumulation is fp32, the output is rounded once.  Range: cached blocks with exponent bytes 3 to 254 (4-bit mantissas) or 3 to 251
+ * (8-bit) exactly, as kvbfp_decode_attention up to 32 heads; larger bytes are taken as the end of that range.  A bias is as exact as fp32:
+ * relative to its own size (where every token that is seen is far away, what they differ by).
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
+size_t kvbfp_scored_workspace_bytes(const kvbfp_layout* layout, int32_t n_q_heads, int32_t n_q_tokens, int64_t max_len);
+int kvbfp_decode_attention_scored(const kvbfp_layout* layout, const kvbfp_cache* cache, int32_t n_q_heads, int32_t n_q_tokens,
+                                  const void* q, kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len,
+                                  float softmax_scale, const int32_t* perm_k, const int32_t* perm_v,
+                                  const kvbfp_score_rule* rule, void* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream);
+/* The same over a pool of pages (arguments of kvbfp_decode_attention_multi_paged). */
+size_t kvbfp_scored_workspace_bytes_paged(const kvbfp_layout* pool, int64_t table_stride, int32_t batch, int32_t n_q_heads,
+                                          int32_t n_q_tokens, int64_t max_len);
+int kvbfp_decode_attention_scored_paged(const kvbfp_layout* pool, const kvbfp_cache* cache, const int32_t* block_table,
+                                        int64_t table_stride, int32_t batch, int32_t n_q_heads, int32_t n_q_tokens,
+                                        const void* q, kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len,
+                                        float softmax_scale, const int32_t* perm_k, const int32_t* perm_v,
+                                        const kvbfp_score_rule* rule, void* out, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* hip_stream);
+
+/* DEVICE, asynchronous.  The attention weights that cached tokens collect, per kv-head:
+ *     weights_out[b][h][t] = decay * weights_in[b][h][t] + sum over the query tokens i and the query heads of kv-head h of exp(y - lse)
+ * with y and the tokens seen as kvbfp_decode_attention_scored has them and the lse that it returned for the same q, rule, scale and
+ * lengths (a row whose lse is -infinity adds nothing).  Reads the keys alone, once.
+ *   lse         : DEVICE float [batch][n_q_tokens][n_q_heads].
+ *   weights_in  : DEVICE float [batch][n_kv_heads][weights_stride], or NULL = zeros (decay is then not looked at).
+ *   weights_out : DEVICE, the same shape; may be weights_in itself.  Tokens from seq_len on are left as they are.
+ *   cache       : the value planes may be NULL.
+ * No atomics: the same bits every time.  Errors: INVALID_ARG (also weights_stride < max_len), UNSUPPORTED, HIP. */
+int kvbfp_accumulate_weights(const kvbfp_layout* layout, const kvbfp_cache* cache, int32_t n_q_heads, int32_t n_q_tokens,
+                             const void* q, kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len,
+                             float softmax_scale, const int32_t* perm_k, const kvbfp_score_rule* rule, const float* lse,
+                             float decay, const float* weights_in, float* weights_out, int64_t weights_stride, void* hip_stream);
+int kvbfp_accumulate_weights_paged(const kvbfp_layout* pool, const kvbfp_cache* cache, const int32_t* block_table,
+                                   int64_t table_stride, int32_t batch, int32_t n_q_heads, int32_t n_q_tokens, const void* q,
+                                   kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len, float softmax_scale,
+                                   const int32_t* perm_k, const kvbfp_score_rule* rule, const float* lse, float decay,
+                                   const float* weights_in, float* weights_out, int64_t weights_stride, void* hip_stream);
+
+/* DEVICE, asynchronous.  Eviction by collected weight: of every sequence and kv-head the first n_first tokens, the last n_recent and, of those
+ * between them, the ones with the largest weights stay, n_keep in all (a sequence of up to n_keep tokens stays whole), and go in their
+ * order to rows 0, 1, .. of another cache, bit for bit.  Equal weights: the lower index stays; NaN counts below everything.
+ * Keys are taken as they are: rotated before they were cached, they keep the angles of their old positions.
+ *   dst_layout, dst : the other cache (same block, mant_bits, n_kv_heads, batch; max_seq >= n_keep); must not overlap the first.  Rows
+ *                     from the new length on are left as they are.
+ *   weights     : DEVICE float [batch][n_kv_heads][weights_stride], as kvbfp_accumulate_weights leaves them.
+ *   kept        : DEVICE int32 [batch][n_kv_heads][n_keep], out: the old index of every token that stays, -1 behind them.
+ *   new_len     : DEVICE int32 [batch], out: min(seq_len, n_keep).  Not seq_len_dev itself.
+ *   weights_out : DEVICE float [batch][n_kv_heads][n_keep] or NULL, out: the weights of the tokens that stay (behind them left as they
+ *                 are).  Must not overlap weights.
+ * Errors: INVALID_ARG (also n_first + n_recent > n_keep), UNSUPPORTED, HIP. */
+int kvbfp_evict(const kvbfp_layout* layout, const kvbfp_cache* cache, const kvbfp_layout* dst_layout, const kvbfp_cache* dst,
+                const float* weights, int64_t weights_stride, const int32_t* seq_len_dev, int64_t max_len, int32_t n_keep,
+                int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* new_len, float* weights_out, void* hip_stream);
+/* The same from a pool of pages to another, or to other pages of the same pool (dst_pool and dst then equal pool and cache; pages that a
+ * sequence is read from must not be among those written: memory-safe, result unspecified). */
+int kvbfp_evict_paged(const kvbfp_layout* pool, const kvbfp_cache* cache, const int32_t* block_table, int64_t table_stride,
+                      int32_t batch, const kvbfp_layout* dst_pool, const kvbfp_cache* dst, const int32_t* dst_table,
+                      int64_t dst_stride, const float* weights, int64_t weights_stride, const int32_t* seq_len_dev,
+                      int64_t max_len, int32_t n_keep, int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* new_len,
+                      float* weights_out, void* hip_stream);
+
 /* Message describing the last error on the calling thread ("" if none).  Static storage. */
 const char* kvbfp_last_error(void);
 

@@ -1,0 +1,287 @@
+// Eviction of cached tokens by the weight they have collected (kvbfp_evict and its paged form): per sequence and kv-head the first n_first
+// tokens, the last n_recent and those with the largest weights between them stay, n_keep in all, and go in their order to another cache.
+//
+// Selection (evict_select), a workgroup per sequence and kv-head: the weight of the last one that stays is found by its bits, eight at
+// a time from the top (a histogram of those that agree in the bits so far), ties go to the lowest index, and what stays is written
+// in order by prefix counts.  Rows (evict_rows): 16 bytes a thread.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "kvbfp_internal.h"
+
+namespace {
+
+constexpr int kD = 128;
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+
+struct EvictArgs {
+    const uint8_t* src[4];               // k_mant, k_exp, v_mant, v_exp
+    uint8_t* dst[4];
+    const int32_t* src_table;
+    const int32_t* dst_table;
+    int64_t src_stride, dst_stride, src_seq, dst_seq;      // tables; tokens of a region
+    int32_t src_log2_page, dst_log2_page, src_pages, dst_pages;
+    const float* weights;                // [B][H][w_stride]
+    int64_t w_stride;
+    const int32_t* seq_len;
+    int32_t max_len, H, batch, n_keep, n_first, n_recent;
+    int32_t* kept;                       // [B][H][n_keep]
+    int32_t* new_len;                    // [B]
+    float* w_out;                        // [B][H][n_keep] or nullptr
+    int32_t mant_bytes, n_exps;          // of a row
+};
+
+__device__ __forceinline__ int length_of(const EvictArgs& a, int b) {
+    return a.seq_len ? min(max(a.seq_len[b], 0), a.max_len) : a.max_len;
+}
+
+// Weights in the order of unsigned integers: NaN lowest, both zeros alike.
+__device__ __forceinline__ uint32_t key_of(float w) {
+    if (w != w) return 0u;
+    const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// grid = (H, B)
+__global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
+    __shared__ int hist_s[256];
+    __shared__ int wave_s[kWaves][2];
+    __shared__ uint32_t prefix_s;
+    __shared__ int left_s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int h = blockIdx.x, b = blockIdx.y;
+    const int len = length_of(a, b), unit = b * a.H + h;
+    const int count = min(len, a.n_keep);
+    int32_t* const kept = a.kept + (int64_t)unit * a.n_keep;
+    if (h == 0 && tid == 0) a.new_len[b] = count;
+    for (int i = count + tid; i < a.n_keep; i += kThreads) kept[i] = -1;
+    if (len <= a.n_keep) {
+        for (int i = tid; i < len; i += kThreads) kept[i] = i;
+        return;
+    }
+    const float* const w = a.weights + (int64_t)unit * a.w_stride;
+    const int lo = a.n_first, hi = len - a.n_recent;       // candidates [lo, hi); more than are needed
+    int need = a.n_keep - a.n_first - a.n_recent;
+    uint32_t bits = 0, known = 0;                          // of the smallest key that stays
+    if (need > 0) {
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 256; i += kThreads) hist_s[i] = 0;
+            __syncthreads();
+            for (int t = lo + tid; t < hi; t += kThreads) {
+                const uint32_t k = key_of(w[t]);
+                if ((k & known) == bits) atomicAdd(&hist_s[(k >> shift) & 255u], 1);
+            }
+            __syncthreads();
+            if (wave == 0) {                               // the digit in which the need-th largest lies: sums from the top
+                int mine[4], total = 0;
+                for (int i = 0; i < 4; ++i) {
+                    mine[i] = hist_s[255 - (4 * lane + i)];
+                    total += mine[i];
+                }
+                int before = total;                        // inclusive sum over the lanes, then exclusive
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int up = __shfl_up(before, d);
+                    if (lane >= d) before += up;
+                }
+                before -= total;
+                for (int i = 0; i < 4; ++i) {
+                    if (before < need && need <= before + mine[i]) {
+                        prefix_s = bits | ((uint32_t)(255 - (4 * lane + i)) << shift);
+                        left_s = need - before;
+                    }
+                    before += mine[i];
+                }
+            }
+            __syncthreads();
+            bits = prefix_s;
+            need = left_s;                                 // of those that agree with `bits`
+            known |= 255u << shift;
+            __syncthreads();
+        }
+    }
+    // in order: every wavefront a stretch of the tokens; what it keeps and how many ties it has, then where they go
+    const int stretch = ((len + kWaves - 1) / kWaves + 63) & ~63;
+    const int from = min(wave * stretch, len), to = min(from + stretch, len);
+    const bool by_weight = a.n_keep - a.n_first - a.n_recent > 0;
+    auto look = [&](int t, bool& more, bool& tie) {
+        more = tie = false;
+        if (t >= to) return;
+        if (t < lo || t >= hi) {
+            more = true;
+            return;
+        }
+        if (!by_weight) return;
+        const uint32_t k = key_of(w[t]);
+        more = k > bits;
+        tie = k == bits;
+    };
+    int n_more = 0, n_tie = 0;
+    for (int t = from; t < to; t += 64) {
+        bool more, tie;
+        look(t + lane, more, tie);
+        n_more += __popcll(__ballot(more));
+        n_tie += __popcll(__ballot(tie));
+    }
+    if (lane == 0) {
+        wave_s[wave][0] = n_more;
+        wave_s[wave][1] = n_tie;
+    }
+    __syncthreads();
+    int at = 0, ties = 0;                                  // places taken, ties seen before this stretch
+    for (int i = 0; i < wave; ++i) {
+        at += wave_s[i][0];
+        ties += wave_s[i][1];
+    }
+    at += min(ties, need);
+    const uint64_t below = (1ull << lane) - 1;
+    for (int t = from; t < to; t += 64) {
+        bool more, tie;
+        look(t + lane, more, tie);
+        const uint64_t all_ties = __ballot(tie);
+        const bool stays = more || (tie && ties + __popcll(all_ties & below) < need);
+        const uint64_t all = __ballot(stays);
+        const int place = at + __popcll(all & below);
+        if (stays && place < a.n_keep) kept[place] = t + lane;
+        at += __popcll(all);
+        ties += __popcll(all_ties);
+    }
+}
+
+__device__ __forceinline__ int64_t row_of(const int32_t* table, int64_t stride, int log2_page, int pages, int64_t seq, int H, int b, int h, int t) {
+    if (!table) return ((int64_t)b * H + h) * seq + t;
+    const int page = min(max(table[(int64_t)b * stride + (t >> log2_page)], 0), pages - 1);
+    return (((int64_t)page * H + h) << log2_page) + (t & ((1 << log2_page) - 1));
+}
+
+// A group of PER threads per kept row: 16 bytes of the key and of the value row each, and the exponents.  grid = (rows / (256 / PER), H, B)
+template <int PER>
+__global__ __launch_bounds__(256) void evict_rows(EvictArgs a) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const int i = (blockIdx.x * 256 + threadIdx.x) / PER, part = threadIdx.x % PER;
+    const int h = blockIdx.y, b = blockIdx.z;
+    if (i >= min(length_of(a, b), a.n_keep)) return;       // (what lies behind the last kept token stays as it was)
+    const int64_t unit = (int64_t)b * a.H + h;
+    const int t = min(max(a.kept[unit * a.n_keep + i], 0), a.max_len - 1);
+    const int64_t from = row_of(a.src_table, a.src_stride, a.src_log2_page, a.src_pages, a.src_seq, a.H, b, h, t);
+    const int64_t to = row_of(a.dst_table, a.dst_stride, a.dst_log2_page, a.dst_pages, a.dst_seq, a.H, b, h, i);
+    const u32x4 k = *(const u32x4*)(a.src[0] + from * (PER * 16) + part * 16);
+    const u32x4 v = *(const u32x4*)(a.src[2] + from * (PER * 16) + part * 16);
+    *(u32x4*)(a.dst[0] + to * (PER * 16) + part * 16) = k;
+    *(u32x4*)(a.dst[2] + to * (PER * 16) + part * 16) = v;
+    for (int e = part; e < a.n_exps; e += PER) {
+        a.dst[1][to * a.n_exps + e] = a.src[1][from * a.n_exps + e];
+        a.dst[3][to * a.n_exps + e] = a.src[3][from * a.n_exps + e];
+    }
+    if (a.w_out && part == 0) a.w_out[unit * a.n_keep + i] = a.weights[unit * a.w_stride + t];
+}
+
+}  // namespace
+
+using namespace kvbfp;
+
+// The planes of a cache that may be written and read share no byte.
+static bool overlap(const void* p, size_t n, const void* q, size_t m) {
+    return (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n;
+}
+
+static int evict_impl(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache, const Paging* paging, const kvbfp_layout* dst_L,
+                      const kvbfp_cache* dst, const Paging* dst_paging, const float* weights, int64_t weights_stride,
+                      const int32_t* seq_len_dev, int64_t max_len, int32_t n_keep, int32_t n_first, int32_t n_recent, int32_t* kept,
+                      int32_t* new_len, float* weights_out, void* hip_stream) {
+    clear_error();
+    kvbfp_layout from, to;
+    if (paging) {
+        if (int rc = check_paging(L, *paging, &from)) return rc;
+        if (int rc = check_paging(dst_L, *dst_paging, &to)) return rc;
+    } else {
+        if (int rc = check_device_layout(L)) return rc;
+        if (int rc = check_device_layout(dst_L)) return rc;
+        from = *L;
+        to = *dst_L;
+    }
+    if (int rc = check_cache(cache, true, true)) return rc;
+    if (int rc = check_cache(dst, true, true)) return rc;
+    if (from.block != to.block || from.mant_bits != to.mant_bits || from.n_kv_heads != to.n_kv_heads || from.batch != to.batch)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: the two caches differ in block, mant_bits, heads or batch", call);
+    if (!weights || !kept || !new_len) return fail(KVBFP_ERR_INVALID_ARG, "%s: weights/kept/new_len is NULL", call);
+    if (max_len <= 0 || max_len > from.max_seq)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: max_len %lld outside (0, max_seq=%lld]", call, (long long)max_len, (long long)from.max_seq);
+    if (weights_stride < max_len)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: weights_stride %lld below max_len %lld", call, (long long)weights_stride, (long long)max_len);
+    if (n_keep <= 0 || n_keep > to.max_seq)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: n_keep %d outside (0, max_seq=%lld] of the cache that it goes to", call, n_keep, (long long)to.max_seq);
+    if (n_first < 0 || n_recent < 0 || (int64_t)n_first + n_recent > n_keep)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: n_first %d and n_recent %d (together at most n_keep = %d)", call, n_first, n_recent, n_keep);
+    if (from.batch > 65535 || from.n_kv_heads > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: batch/heads exceed the grid limits", call);
+    const void* const p[4] = {cache->k_mant, cache->k_exp, cache->v_mant, cache->v_exp};
+    const void* const q[4] = {dst->k_mant, dst->k_exp, dst->v_mant, dst->v_exp};
+    if (paging && std::equal(p, p + 4, q)) {               // other pages of one pool
+        if (L->max_seq != dst_L->max_seq || L->batch != dst_L->batch)
+            return fail(KVBFP_ERR_INVALID_ARG, "%s: one pool with two layouts", call);
+    } else {
+        size_t m[2], e[2];
+        if (int rc = kvbfp_cache_bytes(L, &m[0], &e[0])) return rc;
+        if (int rc = kvbfp_cache_bytes(dst_L, &m[1], &e[1])) return rc;
+        for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < 4; ++j)
+                if (overlap(p[i], i & 1 ? e[0] : m[0], q[j], j & 1 ? e[1] : m[1]))
+                    return fail(KVBFP_ERR_INVALID_ARG, "%s: the two caches overlap", call);
+    }
+    // lengths and weights are read beside the writing of the new ones
+    const size_t units = (size_t)from.batch * (size_t)from.n_kv_heads;
+    if (seq_len_dev && overlap(seq_len_dev, from.batch * sizeof(int32_t), new_len, from.batch * sizeof(int32_t)))
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: new_len overlaps seq_len_dev", call);
+    if (weights_out && overlap(weights, units * (size_t)weights_stride * sizeof(float), weights_out, units * (size_t)n_keep * sizeof(float)))
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: weights_out overlaps weights", call);
+    EvictArgs a{};
+    a.src[0] = cache->k_mant; a.src[1] = cache->k_exp; a.src[2] = cache->v_mant; a.src[3] = cache->v_exp;
+    a.dst[0] = dst->k_mant; a.dst[1] = dst->k_exp; a.dst[2] = dst->v_mant; a.dst[3] = dst->v_exp;
+    a.src_seq = from.max_seq; a.dst_seq = to.max_seq;
+    if (paging) {
+        a.src_table = paging->block_table; a.src_stride = paging->table_stride; a.src_pages = L->batch;
+        a.dst_table = dst_paging->block_table; a.dst_stride = dst_paging->table_stride; a.dst_pages = dst_L->batch;
+        while (((int64_t)1 << a.src_log2_page) < L->max_seq) ++a.src_log2_page;
+        while (((int64_t)1 << a.dst_log2_page) < dst_L->max_seq) ++a.dst_log2_page;
+    }
+    a.weights = weights; a.w_stride = weights_stride; a.seq_len = seq_len_dev;
+    a.max_len = (int32_t)max_len; a.H = from.n_kv_heads; a.batch = from.batch;
+    a.n_keep = n_keep; a.n_first = n_first; a.n_recent = n_recent;
+    a.kept = kept; a.new_len = new_len; a.w_out = weights_out;
+    a.n_exps = kD / from.block;
+    hipStream_t s = (hipStream_t)hip_stream;
+    evict_select<<<dim3((unsigned)a.H, (unsigned)a.batch), kThreads, 0, s>>>(a);
+    hipError_t err = hipGetLastError();
+    if (err == hipSuccess) {
+        const int per = from.mant_bits, rows = 256 / per;                      // 64 or 128 bytes a row
+        const int64_t most = std::min<int64_t>(n_keep, max_len);
+        const dim3 grid((unsigned)((most + rows - 1) / rows), (unsigned)a.H, (unsigned)a.batch);
+        if (per == 4) evict_rows<4><<<grid, 256, 0, s>>>(a);
+        else evict_rows<8><<<grid, 256, 0, s>>>(a);
+        err = hipGetLastError();
+    }
+    if (err != hipSuccess) return fail(KVBFP_ERR_HIP, "%s: %s", call, hipGetErrorString(err));
+    return KVBFP_OK;
+}
+
+extern "C" {
+
+int kvbfp_evict(const kvbfp_layout* L, const kvbfp_cache* cache, const kvbfp_layout* dst_L, const kvbfp_cache* dst, const float* weights,
+                int64_t weights_stride, const int32_t* seq_len_dev, int64_t max_len, int32_t n_keep, int32_t n_first, int32_t n_recent,
+                int32_t* kept, int32_t* new_len, float* weights_out, void* hip_stream) {
+    return evict_impl("evict", L, cache, nullptr, dst_L, dst, nullptr, weights, weights_stride, seq_len_dev, max_len, n_keep, n_first,
+                      n_recent, kept, new_len, weights_out, hip_stream);
+}
+
+int kvbfp_evict_paged(const kvbfp_layout* pool, const kvbfp_cache* cache, const int32_t* block_table, int64_t table_stride, int32_t batch,
+                      const kvbfp_layout* dst_pool, const kvbfp_cache* dst, const int32_t* dst_table, int64_t dst_stride,
+                      const float* weights, int64_t weights_stride, const int32_t* seq_len_dev, int64_t max_len, int32_t n_keep,
+                      int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* new_len, float* weights_out, void* hip_stream) {
+    const Paging pg{block_table, table_stride, batch}, dst_pg{dst_table, dst_stride, batch};
+    return evict_impl("evict_paged", pool, cache, &pg, dst_pool, dst, &dst_pg, weights, weights_stride, seq_len_dev, max_len, n_keep,
+                      n_first, n_recent, kept, new_len, weights_out, hip_stream);
+}
+
+}  // extern "C"

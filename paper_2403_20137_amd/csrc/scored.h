@@ -1,0 +1,293 @@
+// Attention with a rule on its scores, and the weights it gives to cached tokens: argument block, the rule itself and the reading of
+// packed rows, shared by decode_scored.hip and weights.hip (internal, not part of the C ABI).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "decode_dev.h"
+#include "kvbfp_internal.h"
+
+namespace kvbfp {
+namespace scored {
+
+using namespace kvbfp::dev;
+
+struct Args {
+    const uint8_t* k_mant;
+    const uint8_t* k_exp;
+    const uint8_t* v_mant;
+    const uint8_t* v_exp;
+    const void* q;             // [B][n_tok][H_q][D]
+    void* out;                 // the same
+    float* lse;                // [B][n_tok][H_q] or nullptr
+    const int32_t* seq_len;    // [B] or nullptr
+    const int32_t* perm_k;     // [H_kv][D] or nullptr
+    const int32_t* perm_v;
+    float* part_o;             // [B][H_kv][M][n_splits][D], in the order of the positions in LDS (see position_channel)
+    float* part_ml;            // [B][H_kv][M][n_splits][2]: largest score (base 2), sum of the weights relative to it
+    const int32_t* block_table;
+    int64_t table_stride, max_seq;
+    int32_t log2_page, n_pages;
+    int32_t max_len, batch, H_kv, H_q, G, n_tok;
+    int32_t M;                 // rows of a kv-head: query token * G + member of its group
+    int32_t n_splits, row_tiles;
+    int32_t n_exps, log2_block;
+    float score_mul;           // softmax_scale * log2(e): scores are kept in base 2
+    float cap, inv_cap;        // base 2; cap = 0: none
+    const float* slopes;       // [H_q] or nullptr
+    const int32_t* first;      // [B][n_tok] or nullptr
+    const int32_t* prefix;     // [B] or nullptr
+    const uint64_t* tree;      // [B][n_tok] (tree_stride 0: [n_tok], one for all) or nullptr: each token sees those up to itself
+    int32_t tree_stride;
+    int32_t window;            // 0: none
+    // kvbfp_accumulate_weights
+    const float* lse_in;       // [B][n_tok][H_q]
+    const float* w_in;         // [B][H_kv][w_stride] or nullptr
+    float* w_out;
+    int64_t w_stride;
+    float decay;
+};
+
+// What a kernel knows of its sequence.
+struct Seq {
+    int32_t len, base, prefix;           // tokens [base, len) are the last n_tok; base may be negative
+};
+__device__ __forceinline__ Seq sequence(const Args& a, int b) {
+    Seq s;
+    s.len = a.max_len;
+    if (a.seq_len) s.len = min(max(a.seq_len[b], 0), a.max_len);
+    s.base = s.len - a.n_tok;
+    s.prefix = a.prefix ? min(max(a.prefix[b], 0), s.len) : 0;
+    return s;
+}
+
+// Nodes that node i of sequence b sees.
+__device__ __forceinline__ uint64_t node_mask(const Args& a, int b, int i) {
+    if (a.tree) return a.tree[(int64_t)b * a.tree_stride + i];
+    return i >= 63 ? ~0ull : (2ull << i) - 1;
+}
+// Its position behind the tokens before the nodes: how many others it sees.
+__device__ __forceinline__ int node_depth(uint64_t mask, int i) { return __popcll(mask & ~(1ull << i)); }
+
+// The rule for one row (query token, head).
+struct RowRule {
+    uint64_t nodes;
+    int32_t lo;                // tokens before the nodes are seen from here on
+    int32_t first, pos;        // nodes: from `first` on, nearer than the window
+    float slope;               // base 2
+};
+__device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, int kvh, int r) {
+    r = min(r, a.M - 1);
+    const int i = r / a.G, head = kvh * a.G + r - i * a.G;
+    RowRule u;
+    u.nodes = node_mask(a, b, i);
+    u.pos = s.base + node_depth(u.nodes, i);
+    u.first = a.first ? a.first[(int64_t)b * a.n_tok + i] : 0;
+    u.lo = a.window ? max(u.first, u.pos - a.window + 1) : u.first;
+    u.slope = a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
+    return u;
+}
+
+// cap * tanh(y / cap).  Up to 0.35 by the series to x^11 (1.2e-8 relative; the exponential form cancels there), beyond by
+// 1 - 2 / (1 + e^2x).
+__device__ __forceinline__ float capped(float y, float cap, float inv_cap) {
+    const float x = y * inv_cap, z = x * x;
+    float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
+    t = fmaf(z, t, -17.f / 315.f);
+    t = fmaf(z, t, 2.f / 15.f);
+    t = fmaf(z, t, -1.f / 3.f);
+    float v = fmaf(y * z, t, y);
+    const bool far = fabsf(x) > 0.35f;
+    if (__builtin_amdgcn_ballot_w64(far)) {
+        const float e = exp2_raw(fabsf(x) * -2.8853900817779268f);
+        const float h = cap * fmaf(-2.f * e, __builtin_amdgcn_rcpf(1.f + e), 1.f);
+        v = far ? copysignf(h, y) : v;
+    }
+    return v;
+}
+
+// Score (base 2) of token t for a row, -inf where it is not seen.  `inner`: every token of the tile is before the nodes, is
+// seen by every row and lies behind the prefix or not alike.
+template <bool INNER>
+__device__ __forceinline__ float ruled(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, float acc, float mul, int t) {
+    float y = acc * mul;
+    if (a.cap != 0.f) y = capped(y, a.cap, a.inv_cap);
+    if (INNER) {
+        if (a.slopes) y = fmaf(-u.slope, (float)(u.pos - t), y);
+        return y;
+    }
+    const int node = t - s.base;
+    bool seen = t >= u.lo;
+    int far = u.pos - t;
+    if (node >= 0) {
+        far = u.pos - s.base - depth_s[node & 63];
+        seen = ((u.nodes >> (node & 63)) & 1) && t >= u.first && (a.window == 0 || far < a.window);
+    }
+    seen = (seen || t < s.prefix) && t < s.len;
+    if (a.slopes) y = fmaf(-u.slope, fabsf((float)far), y);
+    return seen ? y : -INFINITY;
+}
+
+// 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).
+template <int P, bool N16>
+struct Chunk {
+    u32x4 m[P / 4];
+    uint32_t e[N16 ? 2 : 1];
+};
+template <int P, bool N16>
+__device__ __forceinline__ void load_chunk(const Args& a, const uint8_t* mant, const uint8_t* exps, int64_t row0, int off, int chunk, Chunk<P, N16>& c) {
+    const u32x4* m = (const u32x4*)(mant + row0 * (16 * P) + (uint32_t)(off * (16 * P) + chunk * (4 * P)));
+#pragma unroll
+    for (int i = 0; i < P / 4; ++i) c.m[i] = __builtin_nontemporal_load(m + i);
+    const uint8_t* e = exps + row0 * a.n_exps + (uint32_t)(off * a.n_exps);
+    if (N16) {
+        c.e[0] = e[2 * chunk];
+        c.e[N16 ? 1 : 0] = e[2 * chunk + 1];
+    } else {
+        c.e[0] = e[(chunk * 32) >> a.log2_block];
+    }
+}
+
+// Row of the planes that a stage of 16 tokens (t a multiple of 16, t < len) begins at.  Page numbers come from device memory that the
+// host cannot check: they are clamped to the pool.
+__device__ __forceinline__ int64_t stage_row(const Args& a, int b, int kvh, int t) {
+    if (!a.block_table) return ((int64_t)b * a.H_kv + kvh) * a.max_seq + t;
+    int page = a.block_table[(int64_t)b * a.table_stride + (t >> a.log2_page)];
+    page = min(max(page, 0), a.n_pages - 1);
+    return (((int64_t)page * a.H_kv + kvh) << a.log2_page) + (t & ((1 << a.log2_page) - 1));
+}
+
+// Codes are decoded to bf16 as value * 2^-kShift, exactly for exponent bytes 3 to the largest that fits the conversion's operand; bytes
+// above it are taken as that one, so that a row that is not seen cannot bring an infinity into a product with 0.
+template <int P>
+struct Decode {
+    static constexpr int kShift = P == 4 ? 7 : 3;
+    static constexpr uint32_t kTop = P == 4 ? 254u : 251u;
+};
+template <int P>
+__device__ __forceinline__ uint32_t exp_field(uint32_t e) { return min(e, Decode<P>::kTop) << 23; }
+
+__device__ __forceinline__ uint32_t pack_top(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+
+// Channels [8 j, 8 j + 8) of a chunk as eight bf16, in the order of the conversions (4 bits: even channels, then odd ones).
+template <int P, bool N16>
+__device__ __forceinline__ u32x4 eight(const Chunk<P, N16>& c, int j) {
+    const uint32_t field = exp_field<P>(c.e[N16 ? j >> 1 : 0]);
+    u32x4 r;
+    if constexpr (P == 4) {
+        const Unpacked4 u = unpack8_p4(c.m[0][j], __uint_as_float(field));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, u.p[i]);
+    } else {
+        // a byte s mmmm lll is the sum of the FP8 numbers s000mmmm (eight times the scale) and s0000lll; seven significant bits
+        const float s_lo = __uint_as_float(field), s_hi = __uint_as_float(field + (3u << 23));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t hi, lo;
+            spread8(c.m[j >> 1][(2 * j + h) & 3], hi, lo);
+            const auto h01 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, s_hi, false), h23 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, s_hi, true);
+            const auto l01 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, s_lo, false), l23 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, s_lo, true);
+            r[2 * h] = pack_top(__float_as_uint(h01[0] + l01[0]), __float_as_uint(h01[1] + l01[1]));
+            r[2 * h + 1] = pack_top(__float_as_uint(h23[0] + l23[0]), __float_as_uint(h23[1] + l23[1]));
+        }
+    }
+    return r;
+}
+// Cache channel of position p of a row decoded that way.
+template <int P>
+__host__ __device__ __forceinline__ int position_channel(int p) {
+    if (P == 8) return p;
+    const int x = p & 7;
+    return (p & ~7) | ((x < 4) ? 2 * x : 2 * (x - 4) + 1);
+}
+
+// All-reduce over the four 16-lane rows of a wavefront.
+__device__ __forceinline__ float rows_max(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Puts `rows` query rows from r0 on into q_s[rows][kQStride] as fp32, in the query's own channel order (zeros behind the last row of the
+// kv-head), and the permutation into perm_s[kD].  Called by the whole workgroup; the caller puts a barrier behind it.
+constexpr int kQStride = kD + 4;
+__device__ __forceinline__ void stage_queries(const Args& a, int dt, int b, int kvh, int r0, int rows, float* q_s, int* perm_s) {
+    const int tid = threadIdx.x, nt = blockDim.x;
+    for (int i = tid; i < kD; i += nt) perm_s[i] = a.perm_k ? a.perm_k[kvh * kD + i] & (kD - 1) : i;      // masked: stays inside the row
+    const bool vec = ((uintptr_t)a.q & 15u) == 0;
+    for (int i = tid; i < rows * 16; i += nt) {
+        const int row = i >> 4, c = (i & 15) * 8, r = r0 + row;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r < a.M) {
+            const int tok = r / a.G;
+            const int64_t at = (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
+            if (vec && dt == KVBFP_F32) {
+                const f32x4 lo = *(const f32x4*)((const float*)a.q + at), hi = *(const f32x4*)((const float*)a.q + at + 4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { x[k] = lo[k]; x[4 + k] = hi[k]; }
+            } else if (vec) {
+                const u32x4 w = *(const u32x4*)((const uint16_t*)a.q + at);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t h = (w[k >> 1] >> (16 * (k & 1))) & 0xFFFFu;
+                    x[k] = dt == KVBFP_F16 ? (float)__builtin_bit_cast(_Float16, (unsigned short)h) : __uint_as_float(h << 16);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = load_as_float(a.q, dt, at + k);
+            }
+        }
+        *(f32x4*)(q_s + row * kQStride + c) = f32x4{x[0], x[1], x[2], x[3]};
+        *(f32x4*)(q_s + row * kQStride + c + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    }
+}
+
+// x as QL bf16 numbers whose sum it is: bf16 has one, fp16 8 + 3 bits, fp32 three times 8.
+template <int QL>
+__device__ __forceinline__ void limbs(float x, __bf16 (&l)[QL]) {
+#pragma unroll
+    for (int i = 0; i < QL; ++i) {
+        const uint32_t top = __float_as_uint(x) & 0xFFFF0000u;
+        l[i] = __builtin_bit_cast(__bf16, (unsigned short)(top >> 16));
+        x -= __uint_as_float(top);
+    }
+}
+
+// The query operand of 16 rows: lane (row l % 16, group l / 16), step j: channels 32 group + 8 j .. in the order of eight().
+template <int P, int QL>
+__device__ __forceinline__ void query_operand(const float* q_s, const int* perm_s, int row, int group, bf16x8 (&op)[QL][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            __bf16 l[QL];
+            limbs<QL>(q_s[row * kQStride + perm_s[position_channel<P>(32 * group + 8 * j + x)]], l);
+#pragma unroll
+            for (int i = 0; i < QL; ++i) op[i][j][x] = l[i];
+        }
+    }
+}
+
+// Checks of the arguments that both calls have, and what the kernels need of them (score rule included).
+// `L`: the pool where paging is given.  On success *logical is the layout that the sequences appear to have.
+int fill_args(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache, const Paging* paging, int32_t n_q_heads, int32_t n_q_tokens,
+              const void* q, kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len, float softmax_scale,
+              const kvbfp_score_rule* rule, bool need_v, Args* a, kvbfp_layout* logical);
+
+}  // namespace scored
+}  // namespace kvbfp

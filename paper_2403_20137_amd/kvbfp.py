@@ -29,6 +29,8 @@ EXPORTS = ["kvbfp_cache_bytes", "kvbfp_calibrate_perm", "kvbfp_permute_weights",
            "kvbfp_quantize_append_paged", "kvbfp_dequantize_paged", "kvbfp_decode_workspace_bytes_paged",
            "kvbfp_decode_attention_paged", "kvbfp_append_decode_attention_paged", "kvbfp_decode_attention_multi_paged",
            "kvbfp_decode_attention_noalloc", "kvbfp_measure_stream_read", "kvbfp_decode_attention_profile_ring",
+           "kvbfp_scored_workspace_bytes", "kvbfp_scored_workspace_bytes_paged", "kvbfp_decode_attention_scored",
+           "kvbfp_decode_attention_scored_paged", "kvbfp_accumulate_weights", "kvbfp_accumulate_weights_paged", "kvbfp_evict", "kvbfp_evict_paged",
            "kvbfp_last_error", "kvbfp_version"]
 
 
@@ -47,6 +49,12 @@ class Layout(C.Structure):
 class CachePtrs(C.Structure):
     _fields_ = [("k_mant", C.c_void_p), ("k_exp", C.c_void_p), ("v_mant", C.c_void_p),
                 ("v_exp", C.c_void_p)]
+
+
+class ScoreRule(C.Structure):
+    """kvbfp_score_rule; make_score_rule fills it and keeps the tensors it points at."""
+    _fields_ = [("struct_bytes", C.c_uint32), ("cap", C.c_float), ("window", C.c_int32), ("tree_stride", C.c_int32),
+                ("slopes", C.c_void_p), ("first_dev", C.c_void_p), ("prefix_dev", C.c_void_p), ("tree_mask", C.c_void_p)]
 
 
 _lib = None
@@ -127,6 +135,21 @@ def lib():
         l.kvbfp_decode_attention_noalloc.argtypes = [C.POINTER(Layout), C.POINTER(CachePtrs), C.c_int32, C.c_void_p,
                                                      C.c_int, C.c_void_p, C.c_int64, C.c_float, C.c_void_p,
                                                      C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        _scored = [C.c_int32, C.c_int32, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_float]      # heads .. softmax_scale
+        l.kvbfp_scored_workspace_bytes.restype = C.c_size_t
+        l.kvbfp_scored_workspace_bytes.argtypes = [C.POINTER(Layout), C.c_int32, C.c_int32, C.c_int64]
+        l.kvbfp_scored_workspace_bytes_paged.restype = C.c_size_t
+        l.kvbfp_scored_workspace_bytes_paged.argtypes = [C.POINTER(Layout), C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int64]
+        _attend = _scored + [C.c_void_p, C.c_void_p, C.POINTER(ScoreRule), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        l.kvbfp_decode_attention_scored.argtypes = [C.POINTER(Layout), C.POINTER(CachePtrs)] + _attend
+        l.kvbfp_decode_attention_scored_paged.argtypes = _paged + _attend
+        _collect = _scored + [C.c_void_p, C.POINTER(ScoreRule), C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+        l.kvbfp_accumulate_weights.argtypes = [C.POINTER(Layout), C.POINTER(CachePtrs)] + _collect
+        l.kvbfp_accumulate_weights_paged.argtypes = _paged + _collect
+        _evict = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                  C.c_void_p]
+        l.kvbfp_evict.argtypes = [C.POINTER(Layout), C.POINTER(CachePtrs), C.POINTER(Layout), C.POINTER(CachePtrs)] + _evict
+        l.kvbfp_evict_paged.argtypes = _paged + [C.POINTER(Layout), C.POINTER(CachePtrs), C.c_void_p, C.c_int64] + _evict
         _lib = l
     return _lib
 
@@ -596,6 +619,193 @@ def decode_attention_multi(cache: Cache, q, max_len, softmax_scale, seq_len_dev=
                                               int(q_mant_bits), _dev_ptr(out), _dev_ptr(workspace), workspace.numel(),
                                               _stream_ptr(stream)))
     return out
+
+
+def _rule_tensor(t, what, dtype, dims):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() not in dims or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %s dimensions" % (what, dtype, " or ".join(map(str, dims))))
+    return _dev_ptr(t)
+
+
+def make_score_rule(cap=0.0, slopes=None, window=0, first_dev=None, prefix_dev=None, tree_mask=None) -> ScoreRule:
+    """Rule on the scores (kvbfp_score_rule).  slopes: float32 [n_q_heads]; first_dev: int32 [batch][n_q_tokens]; prefix_dev: int32
+    [batch]; tree_mask: int64 (64 bits) [batch][n_q_tokens], or [n_q_tokens] for one tree for all.  Holds its tensors."""
+    r = ScoreRule(C.sizeof(ScoreRule), float(cap), int(window), 0, _rule_tensor(slopes, "slopes", torch.float32, (1,)),
+                  _rule_tensor(first_dev, "first_dev", torch.int32, (2,)), _rule_tensor(prefix_dev, "prefix_dev", torch.int32, (1,)),
+                  _rule_tensor(tree_mask, "tree_mask", torch.int64, (1, 2)))
+    if tree_mask is not None and tree_mask.dim() == 2:
+        r.tree_stride = tree_mask.shape[1]
+    r.tensors = (slopes, first_dev, prefix_dev, tree_mask)
+    return r
+
+
+def _check_rule(rule, batch, n_tok, n_q_heads):
+    if rule is None:
+        return None
+    slopes, first, prefix, tree = rule.tensors
+    if slopes is not None and slopes.shape[0] != n_q_heads:
+        raise ValueError("slopes must be [n_q_heads]")
+    if first is not None and tuple(first.shape) != (batch, n_tok):
+        raise ValueError("first_dev must be [batch][n_q_tokens]")
+    if prefix is not None and prefix.shape[0] != batch:
+        raise ValueError("prefix_dev must be [batch]")
+    if tree is not None and (tree.shape[-1] != n_tok or (tree.dim() == 2 and tree.shape[0] != batch)):
+        raise ValueError("tree_mask must be [batch][n_q_tokens] or [n_q_tokens]")
+    return C.byref(rule)
+
+
+def _check_queries(q, batch, head_dim):
+    if q.dim() != 4 or not q.is_contiguous() or q.shape[0] != batch or q.shape[3] != head_dim or q.dtype not in _TORCH_DT:
+        raise ValueError("q must be a contiguous [batch][n_q_tokens][n_q_heads][head_dim] tensor")
+
+
+def _check_float(t, what, shape):
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous float32 tensor %s" % (what, list(shape)))
+
+
+def _check_like_q(out, q):
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and type")
+
+
+def _check_lens(seq_len_dev, batch):
+    if seq_len_dev is not None and (tuple(seq_len_dev.shape) != (batch,) or not seq_len_dev.is_contiguous()):
+        raise ValueError("seq_len_dev must be a contiguous int32 tensor [batch]")
+
+
+def scored_workspace_bytes(layout: Layout, n_q_heads, n_q_tokens, max_len) -> int:
+    return int(lib().kvbfp_scored_workspace_bytes(C.byref(layout), int(n_q_heads), int(n_q_tokens), int(max_len)))
+
+
+def scored_workspace_bytes_paged(pool_layout: Layout, pages_per_seq, batch, n_q_heads, n_q_tokens, max_len) -> int:
+    return int(lib().kvbfp_scored_workspace_bytes_paged(C.byref(pool_layout), int(pages_per_seq), int(batch), int(n_q_heads),
+                                                        int(n_q_tokens), int(max_len)))
+
+
+def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_dev, perm_k, perm_v, out, lse, workspace, stream):
+    L = cache.layout
+    _check_queries(q, batch, L.head_dim)
+    n_tok, n_q_heads = q.shape[1], q.shape[2]
+    rule = _check_rule(rule, batch, n_tok, n_q_heads)
+    _check_lens(seq_len_dev, batch)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_like_q(out, q)
+    if lse is not None:
+        _check_float(lse, "lse", q.shape[:3])
+    if workspace is None:
+        need = scored_workspace_bytes(L, n_q_heads, n_tok, max_len) if block_table is None else \
+            scored_workspace_bytes_paged(L, block_table.shape[1], batch, n_q_heads, n_tok, max_len)
+        if need == 0:
+            _check(ERR_INVALID_ARG)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+    ptrs = cache.ptrs
+    rest = (n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
+            _dev_ptr(perm_k, torch.int32), _dev_ptr(perm_v, torch.int32), rule, _dev_ptr(out), _dev_ptr(lse), _dev_ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if block_table is None:
+        _check(lib().kvbfp_decode_attention_scored(C.byref(L), C.byref(ptrs), *rest))
+    else:
+        _check(lib().kvbfp_decode_attention_scored_paged(C.byref(L), C.byref(ptrs), _dev_ptr(block_table), block_table.shape[1], batch, *rest))
+    return out
+
+
+def decode_attention_scored(cache: Cache, q, max_len, softmax_scale, rule=None, seq_len_dev=None, perm_k=None, perm_v=None, out=None,
+                            lse=None, workspace=None, stream=None):
+    """DEVICE, async.  decode_attention_multi with a rule on the scores (make_score_rule); q: [batch][n_q_tokens][n_q_heads][head_dim].
+    lse: float32 [batch][n_q_tokens][n_q_heads] or None, filled.  Returns `out`."""
+    return _scored(cache, None, cache.layout.batch, q, max_len, softmax_scale, rule, seq_len_dev, perm_k, perm_v, out, lse, workspace, stream)
+
+
+def decode_attention_scored_paged(pool: Cache, block_table, q, max_len, softmax_scale, rule=None, seq_len_dev=None, perm_k=None,
+                                  perm_v=None, out=None, lse=None, workspace=None, stream=None):
+    """DEVICE, async.  decode_attention_scored over a pool of pages."""
+    _check_table(block_table, q.shape[0])
+    return _scored(pool, block_table, q.shape[0], q, max_len, softmax_scale, rule, seq_len_dev, perm_k, perm_v, out, lse, workspace, stream)
+
+
+def _accumulate(cache, block_table, batch, q, max_len, softmax_scale, lse, weights_in, weights_out, decay, rule, seq_len_dev, perm_k, stream):
+    L = cache.layout
+    _check_queries(q, batch, L.head_dim)
+    n_tok, n_q_heads = q.shape[1], q.shape[2]
+    rule = _check_rule(rule, batch, n_tok, n_q_heads)
+    _check_lens(seq_len_dev, batch)
+    _check_float(lse, "lse", q.shape[:3])
+    if weights_out is None:
+        weights_out = torch.zeros((batch, L.n_kv_heads, max_len), dtype=torch.float32, device=q.device) if weights_in is None else weights_in
+    if weights_out.dim() != 3:
+        raise ValueError("weights_out must be [batch][n_kv_heads][tokens]")
+    _check_float(weights_out, "weights_out", (batch, L.n_kv_heads, weights_out.shape[2]))
+    if weights_in is not None:
+        _check_float(weights_in, "weights_in", weights_out.shape)
+    ptrs = cache.ptrs
+    rest = (n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
+            _dev_ptr(perm_k, torch.int32), rule, _dev_ptr(lse), float(decay), _dev_ptr(weights_in), _dev_ptr(weights_out),
+            weights_out.shape[2], _stream_ptr(stream))
+    if block_table is None:
+        _check(lib().kvbfp_accumulate_weights(C.byref(L), C.byref(ptrs), *rest))
+    else:
+        _check(lib().kvbfp_accumulate_weights_paged(C.byref(L), C.byref(ptrs), _dev_ptr(block_table), block_table.shape[1], batch, *rest))
+    return weights_out
+
+
+def accumulate_weights(cache: Cache, q, max_len, softmax_scale, lse, weights_in=None, weights_out=None, decay=1.0, rule=None,
+                       seq_len_dev=None, perm_k=None, stream=None):
+    """DEVICE, async.  decay * weights_in + the attention weights that q gives to every cached token; q, lse, rule: those of the
+    decode_attention_scored call.  weights: float32 [batch][n_kv_heads][tokens >= max_len]; weights_out None = in place (zeros without
+    weights_in).  Returns weights_out."""
+    return _accumulate(cache, None, cache.layout.batch, q, max_len, softmax_scale, lse, weights_in, weights_out, decay, rule, seq_len_dev, perm_k, stream)
+
+
+def accumulate_weights_paged(pool: Cache, block_table, q, max_len, softmax_scale, lse, weights_in=None, weights_out=None, decay=1.0,
+                             rule=None, seq_len_dev=None, perm_k=None, stream=None):
+    """DEVICE, async.  accumulate_weights over a pool of pages."""
+    _check_table(block_table, q.shape[0])
+    return _accumulate(pool, block_table, q.shape[0], q, max_len, softmax_scale, lse, weights_in, weights_out, decay, rule, seq_len_dev, perm_k, stream)
+
+
+def _evict_args(batch, heads, weights, max_len, n_keep, n_first, n_recent, kept, new_len, weights_out, seq_len_dev, stream):
+    if weights.dim() != 3:
+        raise ValueError("weights must be [batch][n_kv_heads][tokens]")
+    _check_float(weights, "weights", (batch, heads, weights.shape[2]))
+    if tuple(kept.shape) != (batch, heads, n_keep) or not kept.is_contiguous():
+        raise ValueError("kept must be a contiguous int32 tensor [batch][n_kv_heads][n_keep]")
+    if tuple(new_len.shape) != (batch,) or not new_len.is_contiguous():
+        raise ValueError("new_len must be a contiguous int32 tensor [batch]")
+    if weights_out is not None:
+        _check_float(weights_out, "weights_out", (batch, heads, n_keep))
+    _check_lens(seq_len_dev, batch)
+    return (_dev_ptr(weights), weights.shape[2], _dev_ptr(seq_len_dev, torch.int32), int(max_len), int(n_keep), int(n_first), int(n_recent),
+            _dev_ptr(kept, torch.int32), _dev_ptr(new_len, torch.int32), _dev_ptr(weights_out), _stream_ptr(stream))
+
+
+def evict(cache: Cache, dst: Cache, weights, max_len, n_keep, n_first, n_recent, kept, new_len, weights_out=None, seq_len_dev=None, stream=None):
+    """DEVICE, async.  Moves the n_keep tokens that stay (first n_first, last n_recent, largest weights between) of every sequence and
+    kv-head to `dst`, another cache.  kept: int32 [batch][n_kv_heads][n_keep]; new_len: int32 [batch]; weights_out: float32 like kept, or
+    None.  Returns (kept, new_len)."""
+    L = cache.layout
+    args = _evict_args(L.batch, L.n_kv_heads, weights, max_len, n_keep, n_first, n_recent, kept, new_len, weights_out, seq_len_dev, stream)
+    ptrs, dst_ptrs = cache.ptrs, dst.ptrs
+    _check(lib().kvbfp_evict(C.byref(L), C.byref(ptrs), C.byref(dst.layout), C.byref(dst_ptrs), *args))
+    return kept, new_len
+
+
+def evict_paged(pool: Cache, block_table, dst_pool: Cache, dst_table, weights, max_len, n_keep, n_first, n_recent, kept, new_len,
+                weights_out=None, seq_len_dev=None, stream=None):
+    """DEVICE, async.  evict from a pool of pages to another one, or to other pages of the same."""
+    batch = weights.shape[0]
+    _check_table(block_table, batch)
+    _check_table(dst_table, batch)
+    L = pool.layout
+    args = _evict_args(batch, L.n_kv_heads, weights, max_len, n_keep, n_first, n_recent, kept, new_len, weights_out, seq_len_dev, stream)
+    ptrs, dst_ptrs = pool.ptrs, dst_pool.ptrs
+    _check(lib().kvbfp_evict_paged(C.byref(L), C.byref(ptrs), _dev_ptr(block_table), block_table.shape[1], batch, C.byref(dst_pool.layout),
+                                   C.byref(dst_ptrs), _dev_ptr(dst_table), dst_table.shape[1], *args))
+    return kept, new_len
 
 
 NOALLOC_SCRATCH_BYTES = 4 << 20
