@@ -67,10 +67,10 @@ __device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const b
 }
 
 // One row of the output, or of lse, from its largest score, sum and sums of values.
-__device__ __forceinline__ void store_out(const Args& a, int dt, int64_t at, float v) {
-    if (dt == KVBFP_F32) ((float*)a.out)[at] = v;
-    else if (dt == KVBFP_F16) ((_Float16*)a.out)[at] = (_Float16)v;
-    else ((__bf16*)a.out)[at] = (__bf16)v;
+template <int QL>
+__device__ __forceinline__ void store_out(const Args& a, int64_t at, float v) {
+    typedef typename Io<QL>::T T;
+    ((T*)a.out)[at] = (T)v;
 }
 __device__ __forceinline__ float natural_lse(float m, float l) {
     return l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
@@ -82,7 +82,7 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
 
 // grid = (n_splits, H_kv * row_tiles, B); P mantissa bits, N16 blocks of 16, QL limbs of the query, HC times 16 rows.
 template <int P, bool N16, int QL, int HC>
-__global__ __launch_bounds__(kThreads) void scored_split(Args a, int dt) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(HC == 1 && QL == 1 ? 3 : 2))) void scored_split(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
     __shared__ __align__(16) uint8_t smem[4 * kWaveLds];
     __shared__ float ml_s[4][16][2];
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void scored_split(Args a, int dt) {
     const Seq s = sequence(a, b);
 
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    stage_queries(a, dt, b, kvh, r0, 16 * HC, (float*)smem, perm_s);
+    stage_queries<QL, 16 * HC>(a, b, kvh, r0, (float*)smem, perm_s);
     RowRule u[HC];
     int lo_most = INT32_MIN, lo_least = INT32_MAX;
 #pragma unroll
@@ -177,15 +177,10 @@ __global__ __launch_bounds__(kThreads) void scored_split(Args a, int dt) {
         const bool inner = t0 >= lo_most && t0 + kWaveTokens <= s.base;
 #pragma unroll
         for (int c = 0; c < HC; ++c) {
-            float y[8];
-            float top = -INFINITY;
-            if (inner) {
+            float y[8], top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = ruled<true>(a, s, u[c], depth_s, sc[c][i >> 2][i & 3], mul, t0 + 16 * (i >> 2) + 4 * group + (i & 3));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = ruled<false>(a, s, u[c], depth_s, sc[c][i >> 2][i & 3], mul, t0 + 16 * (i >> 2) + 4 * group + (i & 3));
-            }
+            for (int i = 0; i < 8; ++i) y[i] = sc[c][i >> 2][i & 3] * mul;
+            rule_scores<8>(a, s, u[c], depth_s, inner, t0 + 4 * group, y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
             top = rows_max(top);
@@ -260,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void scored_split(Args a, int dt) {
             for (int i = 0; i < 8; ++i) {
                 int ch = position_channel<P>(p0 + i);
                 if (a.perm_v) ch = a.perm_v[kvh * kD + ch] & (kD - 1);
-                store_out(a, dt, at * kD + ch, acc[i] * by);
+                store_out<QL>(a, at * kD + ch, acc[i] * by);
             }
             if (p0 == 0 && a.lse) a.lse[at] = natural_lse(top, den);
         }
@@ -268,8 +263,8 @@ __global__ __launch_bounds__(kThreads) void scored_split(Args a, int dt) {
 }
 
 // Joins the splits: a wavefront per row, two channels a lane.
-template <int P>
-__global__ __launch_bounds__(kThreads) void scored_combine(Args a, int dt) {
+template <int P, int QL>
+__global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
     const int lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);          // (b * H_kv + kvh) * M + r
     if (row >= (int64_t)a.batch * a.H_kv * a.M) return;
@@ -295,22 +290,29 @@ __global__ __launch_bounds__(kThreads) void scored_combine(Args a, int dt) {
         c0 = a.perm_v[kvh * kD + c0] & (kD - 1);
         c1 = a.perm_v[kvh * kD + c1] & (kD - 1);
     }
-    store_out(a, dt, at * kD + c0, acc.x * by);
-    store_out(a, dt, at * kD + c1, acc.y * by);
+    store_out<QL>(a, at * kD + c0, acc.x * by);
+    store_out<QL>(a, at * kD + c1, acc.y * by);
     if (lane == 0 && a.lse) a.lse[at] = natural_lse(top, den);
 }
 
 template <int P, bool N16, int QL, int HC>
-void launch_split(const Args& a, int dt, hipStream_t s) {
-    scored_split<P, N16, QL, HC><<<dim3((unsigned)a.n_splits, (unsigned)(a.H_kv * a.row_tiles), (unsigned)a.batch), kThreads, 0, s>>>(a, dt);
+void launch_split(const Args& a, hipStream_t s) {
+    scored_split<P, N16, QL, HC><<<dim3((unsigned)a.n_splits, (unsigned)(a.H_kv * a.row_tiles), (unsigned)a.batch), kThreads, 0, s>>>(a);
 }
 template <int P, bool N16>
 void launch_split(const Args& a, int dt, int hc, hipStream_t s) {
-    if (dt == KVBFP_F32) launch_split<P, N16, 3, 1>(a, dt, s);
-    else if (dt == KVBFP_F16 && hc == 1) launch_split<P, N16, 2, 1>(a, dt, s);
-    else if (dt == KVBFP_F16) launch_split<P, N16, 2, 2>(a, dt, s);
-    else if (hc == 1) launch_split<P, N16, 1, 1>(a, dt, s);
-    else launch_split<P, N16, 1, 2>(a, dt, s);
+    if (dt == KVBFP_F32) launch_split<P, N16, 3, 1>(a, s);
+    else if (dt == KVBFP_F16 && hc == 1) launch_split<P, N16, 2, 1>(a, s);
+    else if (dt == KVBFP_F16) launch_split<P, N16, 2, 2>(a, s);
+    else if (hc == 1) launch_split<P, N16, 1, 1>(a, s);
+    else launch_split<P, N16, 1, 2>(a, s);
+}
+
+template <int P>
+void launch_combine(const Args& a, int dt, dim3 grid, hipStream_t s) {
+    if (dt == KVBFP_F32) scored_combine<P, 3><<<grid, kThreads, 0, s>>>(a);
+    else if (dt == KVBFP_F16) scored_combine<P, 2><<<grid, kThreads, 0, s>>>(a);
+    else scored_combine<P, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
 // Rows of a workgroup / 16, and the splits: enough workgroups for three per compute unit, and no more splits than tiles.
@@ -441,8 +443,8 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
     if (err == hipSuccess && a.n_splits > 1) {
         const int64_t rows = (int64_t)a.batch * a.H_kv * a.M;
         const dim3 grid((unsigned)((rows + 3) / 4));
-        if (logical.mant_bits == 4) scored_combine<4><<<grid, kThreads, 0, s>>>(a, (int)dtype);
-        else scored_combine<8><<<grid, kThreads, 0, s>>>(a, (int)dtype);
+        if (logical.mant_bits == 4) launch_combine<4>(a, (int)dtype, grid, s);
+        else launch_combine<8>(a, (int)dtype, grid, s);
         err = hipGetLastError();
     }
     if (err != hipSuccess) return fail(KVBFP_ERR_HIP, "%s: %s", call, hipGetErrorString(err));

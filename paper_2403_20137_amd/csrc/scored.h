@@ -90,44 +90,61 @@ __device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, 
     return u;
 }
 
-// cap * tanh(y / cap).  Up to 0.35 by the series to x^11 (1.2e-8 relative; the exponential form cancels there), beyond by
-// 1 - 2 / (1 + e^2x).
-__device__ __forceinline__ float capped(float y, float cap, float inv_cap) {
-    const float x = y * inv_cap, z = x * x;
-    float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
-    t = fmaf(z, t, -17.f / 315.f);
-    t = fmaf(z, t, 2.f / 15.f);
-    t = fmaf(z, t, -1.f / 3.f);
-    float v = fmaf(y * z, t, y);
-    const bool far = fabsf(x) > 0.35f;
-    if (__builtin_amdgcn_ballot_w64(far)) {
-        const float e = exp2_raw(fabsf(x) * -2.8853900817779268f);
-        const float h = cap * fmaf(-2.f * e, __builtin_amdgcn_rcpf(1.f + e), 1.f);
-        v = far ? copysignf(h, y) : v;
+// y = cap * tanh(y / cap).  Up to 0.35 by the series to x^11 (1.2e-8 relative; the exponential form cancels there), beyond by
+// 1 - 2 / (1 + e^2x), for which one branch asks on behalf of all N scores: most tiles have none.
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_cap) {
+    float most = 0.f, v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float x = y[i] * inv_cap, z = x * x;
+        float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
+        t = fmaf(z, t, -17.f / 315.f);
+        t = fmaf(z, t, 2.f / 15.f);
+        t = fmaf(z, t, -1.f / 3.f);
+        v[i] = fmaf(y[i] * z, t, y[i]);
+        most = fmaxf(most, fabsf(x));
     }
-    return v;
+    constexpr float kSeries = 0.35f;
+    if (__builtin_amdgcn_ballot_w64(most > kSeries)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = fabsf(y[i] * inv_cap);
+            const float e = exp2_raw(x * -2.8853900817779268f);
+            const float h = cap * fmaf(-2.f * e, __builtin_amdgcn_rcpf(1.f + e), 1.f);
+            v[i] = x > kSeries ? copysignf(h, y[i]) : v[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = v[i];
 }
 
-// Score (base 2) of token t for a row, -inf where it is not seen.  `inner`: every token of the tile is before the nodes, is
-// seen by every row and lies behind the prefix or not alike.
-template <bool INNER>
-__device__ __forceinline__ float ruled(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, float acc, float mul, int t) {
-    float y = acc * mul;
-    if (a.cap != 0.f) y = capped(y, a.cap, a.inv_cap);
-    if (INNER) {
-        if (a.slopes) y = fmaf(-u.slope, (float)(u.pos - t), y);
-        return y;
+// Scores (base 2) of one row for the tokens t0 + 16 (i / 4) + i % 4, i < N; -inf where a token is not seen.  `inner`: all of them are
+// seen, and are no nodes.
+template <int N>
+__device__ __forceinline__ void rule_scores(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, bool inner, int t0, float (&y)[N]) {
+    if (a.cap != 0.f) cap_scores<N>(y, a.cap, a.inv_cap);
+    if (inner) {
+        if (a.slopes) {
+            const float far = (float)(u.pos - t0);
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] = fmaf(-u.slope, far - (float)(16 * (i >> 2) + (i & 3)), y[i]);
+        }
+        return;
     }
-    const int node = t - s.base;
-    bool seen = t >= u.lo;
-    int far = u.pos - t;
-    if (node >= 0) {
-        far = u.pos - s.base - depth_s[node & 63];
-        seen = ((u.nodes >> (node & 63)) & 1) && t >= u.first && (a.window == 0 || far < a.window);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int t = t0 + 16 * (i >> 2) + (i & 3), node = t - s.base;
+        bool seen = t >= u.lo;
+        int far = u.pos - t;
+        if (node >= 0) {
+            far = u.pos - s.base - depth_s[node & 63];
+            seen = ((u.nodes >> (node & 63)) & 1) && t >= u.first && (a.window == 0 || far < a.window);
+        }
+        seen = (seen || t < s.prefix) && t < s.len;
+        if (a.slopes) y[i] = fmaf(-u.slope, fabsf((float)far), y[i]);
+        y[i] = seen ? y[i] : -INFINITY;
     }
-    seen = (seen || t < s.prefix) && t < s.len;
-    if (a.slopes) y = fmaf(-u.slope, fabsf((float)far), y);
-    return seen ? y : -INFINITY;
 }
 
 // 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).
@@ -223,37 +240,40 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Puts `rows` query rows from r0 on into q_s[rows][kQStride] as fp32, in the query's own channel order (zeros behind the last row of the
-// kv-head), and the permutation into perm_s[kD].  Called by the whole workgroup; the caller puts a barrier behind it.
+// The element type goes with the number of bf16 numbers that hold one of its values: bf16 one, fp16 two, fp32 three.
+template <int QL>
+struct Io { typedef __bf16 T; };
+template <>
+struct Io<2> { typedef _Float16 T; };
+template <>
+struct Io<3> { typedef float T; };
+
+// Puts ROWS query rows from r0 on into q_s[ROWS][kQStride] as fp32, in the query's own channel order (zeros behind the last row of the
+// kv-head), and the permutation into perm_s[kD].  Called by the whole workgroup of 256; the caller puts a barrier behind it.
 constexpr int kQStride = kD + 4;
-__device__ __forceinline__ void stage_queries(const Args& a, int dt, int b, int kvh, int r0, int rows, float* q_s, int* perm_s) {
-    const int tid = threadIdx.x, nt = blockDim.x;
-    for (int i = tid; i < kD; i += nt) perm_s[i] = a.perm_k ? a.perm_k[kvh * kD + i] & (kD - 1) : i;      // masked: stays inside the row
+template <int QL, int ROWS>
+__device__ __forceinline__ void stage_queries(const Args& a, int b, int kvh, int r0, float* q_s, int* perm_s) {
+    typedef typename Io<QL>::T T;
+    typedef T Tx8 __attribute__((ext_vector_type(8)));
+    const int tid = threadIdx.x;
+    if (tid < kD) perm_s[tid] = a.perm_k ? a.perm_k[kvh * kD + tid] & (kD - 1) : tid;      // masked: stays inside the row
     const bool vec = ((uintptr_t)a.q & 15u) == 0;
-    for (int i = tid; i < rows * 16; i += nt) {
-        const int row = i >> 4, c = (i & 15) * 8, r = r0 + row;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < ROWS / 16; ++p) {
+        const int row = (tid >> 4) + 16 * p, c = (tid & 15) * 8, r = r0 + row;
+        Tx8 x = {0, 0, 0, 0, 0, 0, 0, 0};
         if (r < a.M) {
             const int tok = r / a.G;
-            const int64_t at = (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
-            if (vec && dt == KVBFP_F32) {
-                const f32x4 lo = *(const f32x4*)((const float*)a.q + at), hi = *(const f32x4*)((const float*)a.q + at + 4);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) { x[k] = lo[k]; x[4 + k] = hi[k]; }
-            } else if (vec) {
-                const u32x4 w = *(const u32x4*)((const uint16_t*)a.q + at);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint32_t h = (w[k >> 1] >> (16 * (k & 1))) & 0xFFFFu;
-                    x[k] = dt == KVBFP_F16 ? (float)__builtin_bit_cast(_Float16, (unsigned short)h) : __uint_as_float(h << 16);
-                }
+            const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
+            if (vec) {
+                x = *(const Tx8*)src;
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = load_as_float(a.q, dt, at + k);
+                for (int k = 0; k < 8; ++k) x[k] = src[k];
             }
         }
-        *(f32x4*)(q_s + row * kQStride + c) = f32x4{x[0], x[1], x[2], x[3]};
-        *(f32x4*)(q_s + row * kQStride + c + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        *(f32x4*)(q_s + row * kQStride + c) = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+        *(f32x4*)(q_s + row * kQStride + c + 4) = f32x4{(float)x[4], (float)x[5], (float)x[6], (float)x[7]};
     }
 }
 

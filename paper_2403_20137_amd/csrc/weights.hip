@@ -22,7 +22,7 @@ constexpr int kTileTokens = 128;
 
 // grid = (tiles of 128 tokens, H_kv, B)
 template <int P, bool N16, int QL>
-__global__ __launch_bounds__(kThreads) void accumulate_weights(Args a, int dt) {
+__global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
     __shared__ __align__(16) float q_s[16 * kQStride];
     __shared__ int perm_s[kD];
     __shared__ int depth_s[64];
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a, int dt) {
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < a.M; r0 += 16) {
         __syncthreads();
-        stage_queries(a, dt, b, kvh, r0, 16, q_s, perm_s);
+        stage_queries<QL, 16>(a, b, kvh, r0, q_s, perm_s);
         const int r = r0 + l16;
         const RowRule u = row_rule(a, s, b, kvh, r);
         float lse = -INFINITY;
@@ -70,6 +70,7 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a, int dt) {
         query_operand<P, QL>(q_s, perm_s, l16, group, q);
         const bool counts = lse > -INFINITY;                             // a row that saw nothing has no weights to give
         const float ref = counts ? lse * 1.4426950408889634f : 0.f;
+        float y[8];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             f32x4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -78,11 +79,11 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a, int dt) {
 #pragma unroll
                 for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st][j], q[i][j], sc, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float y = ruled<false>(a, s, u, depth_s, sc[i], mul, t0 + 16 * st + 4 * group + i);
-                acc[4 * st + i] += counts ? exp2_raw(y - ref) : 0.f;
-            }
+            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i] * mul;
         }
+        rule_scores<8>(a, s, u, depth_s, false, t0 + 4 * group, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(y[i] - ref) : 0.f;
     }
     if (!some) return;
     // acc[4 st + i] of the 16 lanes of a group: token t0 + 16 st + 4 group + i
@@ -100,9 +101,9 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a, int dt) {
 template <int P, bool N16>
 void launch(const Args& a, int dt, hipStream_t s) {
     const dim3 grid((unsigned)((a.max_len + kTileTokens - 1) / kTileTokens), (unsigned)a.H_kv, (unsigned)a.batch);
-    if (dt == KVBFP_F32) accumulate_weights<P, N16, 3><<<grid, kThreads, 0, s>>>(a, dt);
-    else if (dt == KVBFP_F16) accumulate_weights<P, N16, 2><<<grid, kThreads, 0, s>>>(a, dt);
-    else accumulate_weights<P, N16, 1><<<grid, kThreads, 0, s>>>(a, dt);
+    if (dt == KVBFP_F32) accumulate_weights<P, N16, 3><<<grid, kThreads, 0, s>>>(a);
+    else if (dt == KVBFP_F16) accumulate_weights<P, N16, 2><<<grid, kThreads, 0, s>>>(a);
+    else accumulate_weights<P, N16, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
