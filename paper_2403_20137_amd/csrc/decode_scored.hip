@@ -25,24 +25,27 @@ using namespace kvbfp::scored;
 
 constexpr int kThreads = 256;
 constexpr int kWaveTokens = 32;
-constexpr int kTileTokens = 128;                 // four wavefronts
+constexpr int kTileTokens = 128;                 // scored_split: four wavefronts
+constexpr int kWideTokens = 64;                  // scored_split_wide: a tile in LDS
 constexpr int kOStride = kD + 4;
 constexpr int kWaveLds = 16 * kOStride * 4;      // 32 rows of values in bf16 (8192 bytes) or 16 rows of outputs in fp32
 
 // The tiles of a sequence that some row of the workgroup sees: those of the prefix, then those from the first token seen on.
+template <int TT>
 struct Tiles {
     int prefix, from, count;
     __device__ __forceinline__ int at(int v) const { return v < prefix ? v : from + (v - prefix); }
 };
-__device__ __forceinline__ Tiles tiles_of(const Seq& s, int lo) {
-    Tiles t;
-    t.prefix = (s.prefix + kTileTokens - 1) / kTileTokens;
-    t.from = max(min(max(lo, 0), max(s.base, 0)) / kTileTokens, t.prefix);
-    t.count = t.prefix + max((s.len + kTileTokens - 1) / kTileTokens - t.from, 0);
+template <int TT>
+__device__ __forceinline__ Tiles<TT> tiles_of(const Seq& s, int lo) {
+    Tiles<TT> t;
+    t.prefix = (s.prefix + TT - 1) / TT;
+    t.from = max(min(max(lo, 0), max(s.base, 0)) / TT, t.prefix);
+    t.count = t.prefix + max((s.len + TT - 1) / TT - t.from, 0);
     return t;
 }
 
-// The value rows of a wavefront in LDS: 256 bytes a token, the eight 32-byte segments of a row exchanged by its number so that 16 rows of
+// Value rows in LDS: 256 bytes a token, the eight 32-byte segments of a row exchanged by its number so that 16 rows of
 // one segment lie in different banks.
 __device__ __forceinline__ int value_at(int row, int seg) { return row * 256 + ((seg ^ (row & 7)) * 32); }
 
@@ -52,9 +55,9 @@ __device__ __forceinline__ s16x4 read_by_channel(const uint8_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
 }
 
-// o += V^T P^T for 32 tokens: lane (row l % 16): probabilities of tokens 4 (l / 16) .. of either stage.
-template <int PL>
-__device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const bf16x8 (&p)[PL], f32x4 (&o)[8]) {
+// o += V^T P^T for 32 tokens and HC times 16 rows: lane (row l % 16): probabilities of tokens 4 (l / 16) .. of either stage.
+template <int PL, int HC>
+__device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const bf16x8 (&p)[HC][PL], f32x4 (&o)[HC][8]) {
     const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2), piece = (i & 3) * 8;
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) {
@@ -62,7 +65,39 @@ __device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const b
         const s16x4 hi = read_by_channel(v_s + value_at(row + 16, ct) + piece);
         const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int l = 0; l < PL; ++l) o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[l], o[ct], 0, 0, 0);
+        for (int c = 0; c < HC; ++c)
+#pragma unroll
+            for (int l = 0; l < PL; ++l) o[c][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[c][l], o[c][ct], 0, 0, 0);
+    }
+}
+
+// Running maximum of one row over the tokens of a tile: the sums follow it.  Returns what the scores are taken relative to.
+__device__ __forceinline__ float follow(float top, float& m, float& l, f32x4 (&o)[8]) {
+    top = rows_max(top);
+    if (__builtin_amdgcn_ballot_w64(top > m)) {
+        const float now = fmaxf(m, top);
+        const float f = now > -INFINITY ? exp2_raw(m - now) : 1.f;
+        m = now;
+        l *= f;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][i] *= f;
+    }
+    return m > -INFINITY ? m : 0.f;
+}
+// Eight scores of a row -> its probabilities as the operand of add_values, and their sum.
+template <int PL>
+__device__ __forceinline__ void probabilities(const float* y, float ref, float& l, bf16x8 (&p)[PL]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float w = exp2_raw(y[i] - ref);
+        l += w;
+        __bf16 lw[PL];
+        limbs<PL>(w, lw);
+        if (PL == 2) lw[1] = (__bf16)(w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));     // rounded, not cut
+#pragma unroll
+        for (int x = 0; x < PL; ++x) p[x][i] = lw[x];
     }
 }
 
@@ -80,159 +115,33 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
     return ((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G);
 }
 
-// grid = (n_splits, H_kv * row_tiles, B); P mantissa bits, N16 blocks of 16, QL limbs of the query, HC times 16 rows.
-template <int P, bool N16, int QL, int HC>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(HC == 1 && QL == 1 ? 3 : 2))) void scored_split(Args a) {
-    constexpr int PL = QL == 3 ? 3 : 2;
-    __shared__ __align__(16) uint8_t smem[4 * kWaveLds];
-    __shared__ float ml_s[4][16][2];
-    __shared__ int perm_s[kD];
-    __shared__ int depth_s[64];
-    static_assert(16 * HC * kQStride * 4 <= 4 * kWaveLds, "the query rows fit");
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l16 = lane & 15, group = lane >> 4;
-    const int b = blockIdx.z, kvh = blockIdx.y / a.row_tiles, r0 = (blockIdx.y % a.row_tiles) * (16 * HC);
-    const int split = blockIdx.x;
-    const Seq s = sequence(a, b);
-
-    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    stage_queries<QL, 16 * HC>(a, b, kvh, r0, (float*)smem, perm_s);
-    RowRule u[HC];
-    int lo_most = INT32_MIN, lo_least = INT32_MAX;
+// The sums of a workgroup's wavefronts for 16 * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
+// 16 (w % RW) ..) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
+// free when this is called.
+template <int P, int QL, int RW>
+__device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int split, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
+                                       const f32x4 (&o)[8], float m, float l) {
+    const int tid = threadIdx.x, l16 = lane & 15, group = lane >> 4;
+    constexpr float up = (float)(1 << Decode<P>::kShift);
+    float* const o_s = (float*)(smem + wave * kWaveLds);
 #pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        u[c] = row_rule(a, s, b, kvh, r0 + 16 * c + l16);
-        lo_most = max(lo_most, u[c].lo);
-        lo_least = min(lo_least, u[c].lo);
+    for (int ct = 0; ct < 8; ++ct) *(f32x4*)(o_s + l16 * kOStride + 16 * ct + 4 * group) = o[ct];
+    const float sum = rows_sum(l);
+    if (group == 0) {
+        ml_s[wave][l16][0] = m;
+        ml_s[wave][l16][1] = sum;
     }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        lo_most = max(lo_most, __shfl_xor(lo_most, d));
-        lo_least = min(lo_least, __shfl_xor(lo_least, d));
-    }
-    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
-    lo_least = __builtin_amdgcn_readfirstlane(lo_least);
     __syncthreads();
-    bf16x8 q[HC][QL][4];
+    const int row = tid >> 4, p0 = (tid & 15) * 8;
 #pragma unroll
-    for (int c = 0; c < HC; ++c) query_operand<P, QL>((const float*)smem, perm_s, 16 * c + l16, group, q[c]);
-    __syncthreads();                                         // the queries give way to the values
-
-    uint8_t* const v_s = smem + wave * kWaveLds;
-    f32x4 o[HC][8];
-    float m[HC], l[HC];
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        m[c] = -INFINITY;
-        l[c] = 0.f;
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) o[c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
-    const Tiles tiles = tiles_of(s, lo_least);
-    const int last16 = (s.len - 1) & ~15;
-    Chunk<P, N16> k_next[2], v_next[2];
-    auto request = [&](int v) {
-        const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
-        if (v >= tiles.count || t0 >= s.len) return;         // (uniform for the wavefront)
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            const int from = min(t0 + 16 * st, last16);
-            const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
-            const int64_t row = stage_row(a, b, kvh, from);
-            load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_next[st]);
-            load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_next[st]);
-        }
-    };
-    request(split);
-    for (int v = split; v < tiles.count; v += a.n_splits) {
-        const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
-        if (t0 >= s.len) break;                              // the wavefront's part of the last tile is empty
-        Chunk<P, N16> kc[2], vc[2];
-#pragma unroll
-        for (int st = 0; st < 2; ++st) { kc[st] = k_next[st]; vc[st] = v_next[st]; }
-        request(v + a.n_splits);
-        // scores
-        f32x4 sc[HC][2];
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-#pragma unroll
-            for (int c = 0; c < HC; ++c) sc[c][st] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 k = __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j));
-#pragma unroll
-                for (int c = 0; c < HC; ++c)
-#pragma unroll
-                    for (int i = 0; i < QL; ++i) sc[c][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][i][j], sc[c][st], 0, 0, 0);
-            }
-        }
-        // values to LDS
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
-        wave_fence();
-        const bool inner = t0 >= lo_most && t0 + kWaveTokens <= s.base;
-#pragma unroll
-        for (int c = 0; c < HC; ++c) {
-            float y[8], top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = sc[c][i >> 2][i & 3] * mul;
-            rule_scores<8>(a, s, u[c], depth_s, inner, t0 + 4 * group, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
-            top = rows_max(top);
-            if (__builtin_amdgcn_ballot_w64(top > m[c])) {
-                const float now = fmaxf(m[c], top);
-                const float f = now > -INFINITY ? exp2_raw(m[c] - now) : 1.f;
-                m[c] = now;
-                l[c] *= f;
-#pragma unroll
-                for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[c][ct][i] *= f;
-            }
-            const float ref = m[c] > -INFINITY ? m[c] : 0.f;
-            bf16x8 p[PL];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float w = exp2_raw(y[i] - ref);
-                l[c] += w;
-                __bf16 lw[PL];
-                limbs<PL>(w, lw);
-                if (PL == 2) lw[1] = (__bf16)(w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));
-#pragma unroll
-                for (int x = 0; x < PL; ++x) p[x][i] = lw[x];
-            }
-            add_values<PL>(v_s, lane, p, o[c]);
-        }
-        wave_fence();
-    }
-
-    // the four wavefronts' sums, 16 rows at a time
-    const float up = (float)(1 << Decode<P>::kShift);
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        if (r0 + 16 * c >= a.M) break;                       // uniform
-        __syncthreads();
-        float* const o_s = (float*)v_s;
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) *(f32x4*)(o_s + l16 * kOStride + 16 * ct + 4 * group) = o[c][ct];
-        const float sum = rows_sum(l[c]);
-        if (group == 0) {
-            ml_s[wave][l16][0] = m[c];
-            ml_s[wave][l16][1] = sum;
-        }
-        __syncthreads();
-        const int row = tid >> 4, p0 = (tid & 15) * 8, r = r0 + 16 * c + row;
+    for (int rw = 0; rw < RW; ++rw) {
+        const int r = r0 + 16 * rw + row;
         if (r >= a.M) continue;
         float top = -INFINITY, den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml_s[w][row][0]);
+        for (int w = rw; w < 4; w += RW) top = fmaxf(top, ml_s[w][row][0]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = rw; w < 4; w += RW) {
             if (!(ml_s[w][row][0] > -INFINITY)) continue;
             const float f = exp2_raw(ml_s[w][row][0] - top);
             den = fmaf(f, ml_s[w][row][1], den);
@@ -259,6 +168,232 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(HC == 
             }
             if (p0 == 0 && a.lse) a.lse[at] = natural_lse(top, den);
         }
+    }
+}
+
+// The rows of the workgroup's heads that matter to what it reads: the first token that some row sees, and from where on all do.
+template <int HC>
+__device__ __forceinline__ void row_limits(const RowRule (&u)[HC], int& least, int& most) {
+    most = INT32_MIN;
+    least = INT32_MAX;
+#pragma unroll
+    for (int c = 0; c < HC; ++c) {
+        most = max(most, u[c].lo);
+        least = min(least, u[c].lo);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        most = max(most, __shfl_xor(most, d));
+        least = min(least, __shfl_xor(least, d));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+}
+
+// Up to 16 rows.  grid = (n_splits, H_kv, B); P mantissa bits, N16 blocks of 16, QL limbs of the query.
+template <int P, bool N16, int QL>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
+    constexpr int PL = QL == 3 ? 3 : 2;
+    __shared__ __align__(16) uint8_t smem[4 * kWaveLds];
+    __shared__ float ml_s[4][16][2];
+    __shared__ int perm_s[kD];
+    __shared__ int depth_s[64];
+    static_assert(16 * kQStride * 4 <= 4 * kWaveLds, "the query rows fit");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, group = lane >> 4;
+    const int b = blockIdx.z, kvh = blockIdx.y, split = blockIdx.x;
+    const Seq s = sequence(a, b);
+
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    stage_queries<QL, 16>(a, b, kvh, 0, (float*)smem, perm_s);
+    const RowRule u[1] = {row_rule(a, s, b, kvh, l16)};
+    int lo_least, lo_most;
+    row_limits<1>(u, lo_least, lo_most);
+    __syncthreads();
+    bf16x8 q[QL][4];
+    query_operand<P, QL>((const float*)smem, perm_s, l16, group, q);
+    __syncthreads();                                         // the queries give way to the values
+
+    uint8_t* const v_s = smem + wave * kWaveLds;
+    f32x4 o[1][8];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) o[0][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    const auto tiles = tiles_of<kTileTokens>(s, lo_least);
+    const int last16 = (s.len - 1) & ~15;
+    Chunk<P, N16> k_next[2], v_next[2];
+    auto request = [&](int v) {
+        const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
+        if (v >= tiles.count || t0 >= s.len) return;         // (uniform for the wavefront)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            const int from = min(t0 + 16 * st, last16);
+            const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
+            const int64_t row = stage_row(a, b, kvh, from);
+            load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_next[st]);
+            load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_next[st]);
+        }
+    };
+    request(split);
+    for (int v = split; v < tiles.count; v += a.n_splits) {
+        const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
+        if (t0 >= s.len) break;                              // the wavefront's part of the last tile is empty
+        Chunk<P, N16> kc[2], vc[2];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) { kc[st] = k_next[st]; vc[st] = v_next[st]; }
+        request(v + a.n_splits);
+        float y[8], top = -INFINITY;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 k = __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j));
+#pragma unroll
+                for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][j], sc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i] * mul;
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
+        wave_fence();
+        rule_scores<8>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
+        const float ref = follow(top, m, l, o[0]);
+        bf16x8 p[1][PL];
+        probabilities<PL>(y, ref, l, p[0]);
+        add_values<PL, 1>(v_s, lane, p, o);
+        wave_fence();
+    }
+    __syncthreads();
+    finish<P, QL, 1>(a, b, kvh, 0, split, smem, ml_s, wave, lane, o[0], m, l);
+}
+
+// More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
+// (the rows of a workgroup: 16 * RW * HC) and the 4 / RW that have the same ones share the tokens of a tile out.  While one half of
+// the LDS is multiplied with, the next tile is decoded into the other and the one after it is requested: one barrier a tile.
+// grid = (n_splits, H_kv * row_tiles, B).
+template <int P, bool N16, int QL, int HC, int RW>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void scored_split_wide(Args a) {
+    constexpr int PL = QL == 3 ? 3 : 2;
+    constexpr int KS = RW / 2;                               // steps of 32 tokens per wavefront and tile
+    constexpr int kPlane = kWideTokens * 256, kTile = 2 * kPlane;      // keys, values
+    __shared__ __align__(16) uint8_t smem[2 * kTile];
+    __shared__ float ml_s[4][16][2];
+    __shared__ int perm_s[kD];
+    __shared__ int depth_s[64];
+    static_assert(16 * RW * kQStride * 4 <= 2 * kTile && 4 * kWaveLds <= 2 * kTile, "the query rows and the sums fit");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, group = lane >> 4;
+    const int b = blockIdx.z, kvh = blockIdx.y / a.row_tiles, r0 = (blockIdx.y % a.row_tiles) * (16 * HC * RW), split = blockIdx.x;
+    const int rw = wave % RW, part = wave / RW;              // its rows; its part of a tile's tokens
+    const Seq s = sequence(a, b);
+
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    RowRule u[HC];
+    bf16x8 q[HC][QL][4];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) {
+        u[c] = row_rule(a, s, b, kvh, r0 + 16 * (RW * c + rw) + l16);
+        if (c > 0) __syncthreads();
+        stage_queries<QL, 16 * RW>(a, b, kvh, r0 + 16 * RW * c, (float*)smem, perm_s);
+        __syncthreads();
+        query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[c]);
+    }
+    int lo_least, lo_most;
+    row_limits<HC>(u, lo_least, lo_most);
+    if (lane == 0) ml_s[0][wave][0] = __int_as_float(lo_least);        // (as bits) tiles are the workgroup's, not the wavefront's
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) lo_least = min(lo_least, __float_as_int(ml_s[0][w][0]));
+    lo_least = __builtin_amdgcn_readfirstlane(lo_least);
+
+    f32x4 o[HC][8];
+    float m[HC], l[HC];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) {
+        m[c] = -INFINITY;
+        l[c] = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) o[c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    const auto tiles = tiles_of<kWideTokens>(s, lo_least);
+    const int last16 = (s.len - 1) & ~15;
+    // a thread decodes 32 channels of one token, keys and values: wavefront w tokens 16 w ..
+    Chunk<P, N16> k_raw, v_raw;
+    auto request = [&](int v) {
+        if (v >= tiles.count) return;
+        const int t0 = tiles.at(v) * kWideTokens + 16 * wave, from = min(t0, last16);
+        const int off = min(t0 + l16, s.len - 1) - from;
+        const int64_t row = stage_row(a, b, kvh, from);
+        load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_raw);
+        load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_raw);
+    };
+    auto key_at = [](int row, int piece) { return row * 256 + ((piece ^ (row & 15)) * 16); };
+    auto decode = [&](uint8_t* tile) {
+        const int row = 16 * wave + l16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(u32x4*)(tile + key_at(row, 4 * group + j)) = eight<P, N16>(k_raw, j);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(v_raw, j);
+    };
+    request(split);
+    if (split < tiles.count) decode(smem);
+    request(split + a.n_splits);
+    int half = 0;
+    for (int v = split; v < tiles.count; v += a.n_splits, half ^= 1) {
+        __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
+        const uint8_t* const tile = smem + half * kTile;
+        if (v + a.n_splits < tiles.count) decode(smem + (half ^ 1) * kTile);
+        request(v + 2 * a.n_splits);
+        // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
+#pragma unroll 1
+        for (int ks = 0; ks < KS; ++ks) {
+            const int row = 32 * (KS * part + ks), t0 = tiles.at(v) * kWideTokens + row;
+            float y[HC][8];
+#pragma unroll
+            for (int ts = 0; ts < 2; ++ts) {
+                f32x4 sc[HC];
+#pragma unroll
+                for (int c = 0; c < HC; ++c) sc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 k = *(const bf16x8*)(tile + key_at(row + 16 * ts + l16, 4 * group + j));
+#pragma unroll
+                    for (int c = 0; c < HC; ++c)
+#pragma unroll
+                        for (int i = 0; i < QL; ++i) sc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][i][j], sc[c], 0, 0, 0);
+                }
+#pragma unroll
+                for (int c = 0; c < HC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[c][4 * ts + i] = sc[c][i] * mul;
+            }
+            const bool inner = t0 >= lo_most && t0 + 32 <= s.base;
+            bf16x8 p[HC][PL];
+#pragma unroll
+            for (int c = 0; c < HC; ++c) {
+                float top = -INFINITY;
+                rule_scores<8>(a, s, u[c], depth_s, inner, t0 + 4 * group, y[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, y[c][i]);
+                const float ref = follow(top, m[c], l[c], o[c]);
+                probabilities<PL>(y[c], ref, l[c], p[c]);
+            }
+            add_values<PL, HC>(tile + kPlane + row * 256, lane, p, o);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < HC; ++c) {
+        __syncthreads();
+        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, split, smem, ml_s, wave, lane, o[c], m[c], l[c]);
     }
 }
 
@@ -295,17 +430,23 @@ __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
     if (lane == 0 && a.lse) a.lse[at] = natural_lse(top, den);
 }
 
-template <int P, bool N16, int QL, int HC>
-void launch_split(const Args& a, hipStream_t s) {
-    scored_split<P, N16, QL, HC><<<dim3((unsigned)a.n_splits, (unsigned)(a.H_kv * a.row_tiles), (unsigned)a.batch), kThreads, 0, s>>>(a);
+// Rows of a workgroup: 16 in scored_split, 16 * rw * hc in scored_split_wide; splits: enough workgroups for the compute units, and no
+// more than there are tiles.
+struct Plan { int32_t hc, rw, row_tiles, n_splits; };
+
+template <int P, bool N16, int QL>
+void launch_split(const Args& a, const Plan& p, hipStream_t s) {
+    const dim3 grid((unsigned)a.n_splits, (unsigned)(a.H_kv * a.row_tiles), (unsigned)a.batch);
+    if (p.rw == 1) scored_split<P, N16, QL><<<grid, kThreads, 0, s>>>(a);
+    else if (p.rw == 2) scored_split_wide<P, N16, QL, 1, 2><<<grid, kThreads, 0, s>>>(a);
+    else if (QL == 3 || p.hc == 1) scored_split_wide<P, N16, QL, 1, 4><<<grid, kThreads, 0, s>>>(a);
+    else scored_split_wide<P, N16, QL, QL == 3 ? 1 : 2, 4><<<grid, kThreads, 0, s>>>(a);
 }
 template <int P, bool N16>
-void launch_split(const Args& a, int dt, int hc, hipStream_t s) {
-    if (dt == KVBFP_F32) launch_split<P, N16, 3, 1>(a, s);
-    else if (dt == KVBFP_F16 && hc == 1) launch_split<P, N16, 2, 1>(a, s);
-    else if (dt == KVBFP_F16) launch_split<P, N16, 2, 2>(a, s);
-    else if (hc == 1) launch_split<P, N16, 1, 1>(a, s);
-    else launch_split<P, N16, 1, 2>(a, s);
+void launch_split(const Args& a, int dt, const Plan& p, hipStream_t s) {
+    if (dt == KVBFP_F32) launch_split<P, N16, 3>(a, p, s);
+    else if (dt == KVBFP_F16) launch_split<P, N16, 2>(a, p, s);
+    else launch_split<P, N16, 1>(a, p, s);
 }
 
 template <int P>
@@ -315,23 +456,24 @@ void launch_combine(const Args& a, int dt, dim3 grid, hipStream_t s) {
     else scored_combine<P, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
-// Rows of a workgroup / 16, and the splits: enough workgroups for three per compute unit, and no more splits than tiles.
-struct Plan { int32_t hc, row_tiles, n_splits; };
 Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
     Plan p;
-    p.hc = rows > 16 ? 2 : 1;
-    p.row_tiles = (int32_t)((rows + 16 * p.hc - 1) / (16 * p.hc));
+    p.hc = rows > 64 ? 2 : 1;
+    p.rw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int64_t of_wg = 16 * p.hc * p.rw;
+    p.row_tiles = (int32_t)((rows + of_wg - 1) / of_wg);
     const int64_t units = (int64_t)L->batch * L->n_kv_heads * p.row_tiles;
-    const int64_t tiles = (max_len + kTileTokens - 1) / kTileTokens;
-    p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (768 + units - 1) / units));
+    const int64_t tile = p.rw == 1 ? kTileTokens : kWideTokens, tiles = (max_len + tile - 1) / tile;
+    const int64_t wanted = p.rw == 1 ? 768 : 512;
+    p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (wanted + units - 1) / units));
     return p;
 }
-// fp32 I/O takes 16 rows a workgroup: its plan is the one that needs more room.
+// The splits, and with them the workspace, do not depend on the type; fp32 I/O has 64 rows a workgroup at most.
 Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
     Plan p = plan(L, rows, max_len);
     if (dtype == KVBFP_F32 && p.hc == 2) {
         p.hc = 1;
-        p.row_tiles = (int32_t)((rows + 15) / 16);
+        p.row_tiles = (int32_t)((rows + 63) / 64);
     }
     return p;
 }
@@ -433,11 +575,11 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
     hipStream_t s = (hipStream_t)hip_stream;
     const bool n16 = logical.block == 16;
     if (logical.mant_bits == 4) {
-        if (n16) launch_split<4, true>(a, (int)dtype, p.hc, s);
-        else launch_split<4, false>(a, (int)dtype, p.hc, s);
+        if (n16) launch_split<4, true>(a, (int)dtype, p, s);
+        else launch_split<4, false>(a, (int)dtype, p, s);
     } else {
-        if (n16) launch_split<8, true>(a, (int)dtype, p.hc, s);
-        else launch_split<8, false>(a, (int)dtype, p.hc, s);
+        if (n16) launch_split<8, true>(a, (int)dtype, p, s);
+        else launch_split<8, false>(a, (int)dtype, p, s);
     }
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && a.n_splits > 1) {
