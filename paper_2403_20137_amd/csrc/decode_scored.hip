@@ -119,7 +119,7 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
 // 16 (w % RW) ..) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
 // free when this is called.
 template <int P, int QL, int RW>
-__device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int split, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
+__device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int place, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
                                        const f32x4 (&o)[8], float m, float l) {
     const int tid = threadIdx.x, l16 = lane & 15, group = lane >> 4;
     constexpr float up = (float)(1 << Decode<P>::kShift);
@@ -150,7 +150,7 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
             for (int i = 0; i < 8; ++i) acc[i] = fmaf(f, src[i], acc[i]);
         }
         if (a.n_splits > 1) {
-            const int64_t at = (((int64_t)b * a.H_kv + kvh) * a.M + r) * a.n_splits + split;
+            const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
             if (p0 == 0) {
                 a.part_ml[2 * at] = top;
                 a.part_ml[2 * at + 1] = den;
@@ -190,7 +190,7 @@ __device__ __forceinline__ void row_limits(const RowRule (&u)[HC], int& least, i
     least = __builtin_amdgcn_readfirstlane(least);
 }
 
-// Up to 16 rows.  grid = (n_splits, H_kv, B); P mantissa bits, N16 blocks of 16, QL limbs of the query.
+// Up to 16 rows.  grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL limbs of the query.
 template <int P, bool N16, int QL>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
@@ -201,7 +201,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     static_assert(16 * kQStride * 4 <= 4 * kWaveLds, "the query rows fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
-    const int b = blockIdx.z, kvh = blockIdx.y, split = blockIdx.x;
+    const Place place = place_at(a, blockIdx.x);
+    if (place.split < 0) return;
+    const int b = place.b, kvh = blockIdx.y, split = place.split, n_splits = place.n;
     const Seq s = sequence(a, b);
 
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
@@ -236,13 +238,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         }
     };
     request(split);
-    for (int v = split; v < tiles.count; v += a.n_splits) {
+    for (int v = split; v < tiles.count; v += n_splits) {
         const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
         if (t0 >= s.len) break;                              // the wavefront's part of the last tile is empty
         Chunk<P, N16> kc[2], vc[2];
 #pragma unroll
         for (int st = 0; st < 2; ++st) { kc[st] = k_next[st]; vc[st] = v_next[st]; }
-        request(v + a.n_splits);
+        request(v + n_splits);
         float y[8], top = -INFINITY;
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             for (int j = 0; j < 4; ++j)
                 *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
         wave_fence();
-        rule_scores<8>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, y);
+        rule_scores<8, QL == 3>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
         const float ref = follow(top, m, l, o[0]);
@@ -272,13 +274,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         wave_fence();
     }
     __syncthreads();
-    finish<P, QL, 1>(a, b, kvh, 0, split, smem, ml_s, wave, lane, o[0], m, l);
+    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], m, l);
 }
 
 // More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
 // (the rows of a workgroup: 16 * RW * HC) and the 4 / RW that have the same ones share the tokens of a tile out.  While one half of
 // the LDS is multiplied with, the next tile is decoded into the other and the one after it is requested: one barrier a tile.
-// grid = (n_splits, H_kv * row_tiles, B).
+// grid = (n_splits * B, H_kv * row_tiles).
 template <int P, bool N16, int QL, int HC, int RW>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void scored_split_wide(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
@@ -291,7 +293,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     static_assert(16 * RW * kQStride * 4 <= 2 * kTile && 4 * kWaveLds <= 2 * kTile, "the query rows and the sums fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
-    const int b = blockIdx.z, kvh = blockIdx.y / a.row_tiles, r0 = (blockIdx.y % a.row_tiles) * (16 * HC * RW), split = blockIdx.x;
+    const Place place = place_at(a, blockIdx.x);
+    if (place.split < 0) return;
+    const int b = place.b, split = place.split, n_splits = place.n;
+    const int kvh = blockIdx.y / a.row_tiles, r0 = (blockIdx.y % a.row_tiles) * (16 * HC * RW);
     const int rw = wave % RW, part = wave / RW;              // its rows; its part of a tile's tokens
     const Seq s = sequence(a, b);
 
@@ -346,13 +351,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     };
     request(split);
     if (split < tiles.count) decode(smem);
-    request(split + a.n_splits);
+    request(split + n_splits);
     int half = 0;
-    for (int v = split; v < tiles.count; v += a.n_splits, half ^= 1) {
+    for (int v = split; v < tiles.count; v += n_splits, half ^= 1) {
         __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
-        if (v + a.n_splits < tiles.count) decode(smem + (half ^ 1) * kTile);
-        request(v + 2 * a.n_splits);
+        if (v + n_splits < tiles.count) decode(smem + (half ^ 1) * kTile);
+        request(v + 2 * n_splits);
         // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
 #pragma unroll 1
         for (int ks = 0; ks < KS; ++ks) {
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
             for (int c = 0; c < HC; ++c) {
                 float top = -INFINITY;
-                rule_scores<8>(a, s, u[c], depth_s, inner, t0 + 4 * group, y[c]);
+                rule_scores<8, QL == 3>(a, s, u[c], depth_s, inner, t0 + 4 * group, y[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, y[c][i]);
                 const float ref = follow(top, m[c], l[c], o[c]);
@@ -393,38 +398,74 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int c = 0; c < HC; ++c) {
         __syncthreads();
-        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, split, smem, ml_s, wave, lane, o[c], m[c], l[c]);
+        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, blockIdx.x, smem, ml_s, wave, lane, o[c], m[c], l[c]);
     }
 }
 
-// Joins the splits: a wavefront per row, two channels a lane.
-template <int P, int QL>
+// Joins the splits: WPR wavefronts per row (1 or 4, which take every fourth split), two channels a lane, sixteen partial results in flight.
+template <int P, int QL, int WPR>
 __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);          // (b * H_kv + kvh) * M + r
+    __shared__ float join_s[4][64][4];
+    constexpr int kFly = 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + wave / WPR;          // (b * H_kv + kvh) * M + r
     if (row >= (int64_t)a.batch * a.H_kv * a.M) return;
-    const int unit = (int)(row / a.M), r = (int)(row - (int64_t)unit * a.M), b = unit / a.H_kv, kvh = unit % a.H_kv;
-    const int64_t first = row * a.n_splits;
-    float top = -INFINITY, den = 0.f;
-    float2 acc = {0.f, 0.f};
-    for (int i = 0; i < a.n_splits; ++i) top = fmaxf(top, a.part_ml[2 * (first + i)]);
-    if (top > -INFINITY) {
-        for (int i = 0; i < a.n_splits; ++i) {
-            const float f = exp2_raw(a.part_ml[2 * (first + i)] - top);
-            if (f == 0.f) continue;                           // a split that saw nothing
-            den = fmaf(f, a.part_ml[2 * (first + i) + 1], den);
-            const float2 v = *(const float2*)(a.part_o + (first + i) * kD + 2 * lane);
-            acc.x = fmaf(f, v.x, acc.x);
-            acc.y = fmaf(f, v.y, acc.y);
-        }
-    }
-    const float by = den > 0.f ? 1.f / den : 0.f;
-    const int64_t at = out_row(a, b, kvh, r);
+    const int unit = (int)(row / a.M), r = (int)(row - (int64_t)unit * a.M), b = unit / a.H_kv, kvh = unit - b * a.H_kv;
+    const Place place = places_of(a, b);
+    const int64_t first = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place.first;
     int c0 = position_channel<P>(2 * lane), c1 = position_channel<P>(2 * lane + 1);
     if (a.perm_v) {
         c0 = a.perm_v[kvh * kD + c0] & (kD - 1);
         c1 = a.perm_v[kvh * kD + c1] & (kD - 1);
     }
+    float top = -INFINITY, den = 0.f;
+    float2 acc = {0.f, 0.f};
+    const int part = wave % WPR;
+    for (int i0 = part; i0 < place.n; i0 += kFly * WPR) {
+        float2 v[kFly];
+        const int mine = i0 + (lane & (kFly - 1)) * WPR;
+        float2 ml = *(const float2*)(a.part_ml + 2 * (first + min(mine, place.n - 1)));
+        if (mine >= place.n) ml.x = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kFly; ++i)
+            if (i0 + i * WPR < place.n) v[i] = *(const float2*)(a.part_o + (first + i0 + i * WPR) * kD + 2 * lane);      // (uniform)
+        float now = fmaxf(top, row_max(ml.x));
+        const float ref = now > -INFINITY ? now : 0.f;
+        const float w = exp2_raw(ml.x - ref), was = exp2_raw(top - ref);       // 0 for a split that saw nothing
+        top = now;
+        den = fmaf(den, was, row_sum(w * ml.y));
+        acc.x *= was;
+        acc.y *= was;
+#pragma unroll
+        for (int i = 0; i < kFly; ++i) {
+            if (i0 + i * WPR < place.n) {
+                const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+                acc.x = fmaf(wi, v[i].x, acc.x);
+                acc.y = fmaf(wi, v[i].y, acc.y);
+            }
+        }
+    }
+    if (WPR > 1) {
+        *(f32x4*)join_s[wave][lane] = f32x4{top, den, acc.x, acc.y};
+        __syncthreads();
+        if (part) return;
+        float all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) all = fmaxf(all, join_s[w][lane][0]);
+        const float ref = all > -INFINITY ? all : 0.f;
+        top = all;
+        den = acc.x = acc.y = 0.f;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) {
+            const f32x4 x = *(const f32x4*)join_s[w][lane];
+            const float f = exp2_raw(x[0] - ref);
+            den = fmaf(f, x[1], den);
+            acc.x = fmaf(f, x[2], acc.x);
+            acc.y = fmaf(f, x[3], acc.y);
+        }
+    }
+    const float by = den > 0.f ? 1.f / den : 0.f;
+    const int64_t at = out_row(a, b, kvh, r);
     store_out<QL>(a, at * kD + c0, acc.x * by);
     store_out<QL>(a, at * kD + c1, acc.y * by);
     if (lane == 0 && a.lse) a.lse[at] = natural_lse(top, den);
@@ -436,7 +477,7 @@ struct Plan { int32_t hc, rw, row_tiles, n_splits; };
 
 template <int P, bool N16, int QL>
 void launch_split(const Args& a, const Plan& p, hipStream_t s) {
-    const dim3 grid((unsigned)a.n_splits, (unsigned)(a.H_kv * a.row_tiles), (unsigned)a.batch);
+    const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)(a.H_kv * a.row_tiles));
     if (p.rw == 1) scored_split<P, N16, QL><<<grid, kThreads, 0, s>>>(a);
     else if (p.rw == 2) scored_split_wide<P, N16, QL, 1, 2><<<grid, kThreads, 0, s>>>(a);
     else if (QL == 3 || p.hc == 1) scored_split_wide<P, N16, QL, 1, 4><<<grid, kThreads, 0, s>>>(a);
@@ -449,11 +490,18 @@ void launch_split(const Args& a, int dt, const Plan& p, hipStream_t s) {
     else launch_split<P, N16, 1>(a, p, s);
 }
 
+// Few rows with many splits: four wavefronts for each.
+template <int P, int QL>
+void launch_combine(const Args& a, hipStream_t s) {
+    const int64_t rows = (int64_t)a.batch * a.H_kv * a.M;
+    if (a.n_splits > 4 && rows <= 2048) scored_combine<P, QL, 4><<<dim3((unsigned)rows), kThreads, 0, s>>>(a);
+    else scored_combine<P, QL, 1><<<dim3((unsigned)((rows + 3) / 4)), kThreads, 0, s>>>(a);
+}
 template <int P>
-void launch_combine(const Args& a, int dt, dim3 grid, hipStream_t s) {
-    if (dt == KVBFP_F32) scored_combine<P, 3><<<grid, kThreads, 0, s>>>(a);
-    else if (dt == KVBFP_F16) scored_combine<P, 2><<<grid, kThreads, 0, s>>>(a);
-    else scored_combine<P, 1><<<grid, kThreads, 0, s>>>(a);
+void launch_combine(const Args& a, int dt, hipStream_t s) {
+    if (dt == KVBFP_F32) launch_combine<P, 3>(a, s);
+    else if (dt == KVBFP_F16) launch_combine<P, 2>(a, s);
+    else launch_combine<P, 1>(a, s);
 }
 
 Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
@@ -568,6 +616,7 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
     if (need && (uintptr_t)workspace % 256 != 0) return fail(KVBFP_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", call);
     a.out = out; a.lse = lse; a.perm_k = perm_k; a.perm_v = perm_v;
     a.n_splits = p.n_splits; a.row_tiles = p.row_tiles;
+    a.share = seq_len_dev && a.batch > 1 && a.batch <= 64 && p.n_splits > 1;
     if (need) {
         a.part_o = (float*)workspace;
         a.part_ml = a.part_o + (size_t)a.batch * a.H_kv * a.M * a.n_splits * kD;
@@ -583,10 +632,8 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
     }
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && a.n_splits > 1) {
-        const int64_t rows = (int64_t)a.batch * a.H_kv * a.M;
-        const dim3 grid((unsigned)((rows + 3) / 4));
-        if (logical.mant_bits == 4) launch_combine<4>(a, (int)dtype, grid, s);
-        else launch_combine<8>(a, (int)dtype, grid, s);
+        if (logical.mant_bits == 4) launch_combine<4>(a, (int)dtype, s);
+        else launch_combine<8>(a, (int)dtype, s);
         err = hipGetLastError();
     }
     if (err != hipSuccess) return fail(KVBFP_ERR_HIP, "%s: %s", call, hipGetErrorString(err));

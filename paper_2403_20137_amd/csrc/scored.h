@@ -25,14 +25,15 @@ struct Args {
     const int32_t* seq_len;    // [B] or nullptr
     const int32_t* perm_k;     // [H_kv][D] or nullptr
     const int32_t* perm_v;
-    float* part_o;             // [B][H_kv][M][n_splits][D], in the order of the positions in LDS (see position_channel)
-    float* part_ml;            // [B][H_kv][M][n_splits][2]: largest score (base 2), sum of the weights relative to it
+    float* part_o;             // [H_kv][M][n_splits * B][D], in the order of the positions in LDS (see position_channel)
+    float* part_ml;            // [H_kv][M][n_splits * B][2]: largest score (base 2), sum of the weights relative to it
     const int32_t* block_table;
     int64_t table_stride, max_seq;
     int32_t log2_page, n_pages;
     int32_t max_len, batch, H_kv, H_q, G, n_tok;
     int32_t M;                 // rows of a kv-head: query token * G + member of its group
     int32_t n_splits, row_tiles;
+    int32_t share;             // the n_splits * B places of a kv-head are shared out by the lengths
     int32_t n_exps, log2_block;
     float score_mul;           // softmax_scale * log2(e): scores are kept in base 2
     float cap, inv_cap;        // base 2; cap = 0: none
@@ -63,6 +64,66 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
     return s;
 }
 
+// Which part of which sequence a place takes: part `split` of `n`, the places of the sequence begin at `first`.  Equal parts
+// (n_splits each), or shared out by what the sequences have to read (up to 64 of them, a lane each): one each, the others in
+// proportion.  (Rounded down, so that all fit: the sum of rounded-down shares is at most what there is to share.)
+struct Place { int b, split, n, first; };
+__device__ __forceinline__ int tokens_read(const Args& a, int b) {        // about: documents are not looked at
+    int len = min(max(a.seq_len[b], 0), a.max_len);
+    if (a.window) {
+        const int near = a.window + a.n_tok + (a.prefix ? min(max(a.prefix[b], 0), len) : 0);
+        len = min(len, near);
+    }
+    return len;
+}
+__device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first) {
+    const float mine = lane < a.batch ? (float)(tokens_read(a, lane) + 1) : 0.f;
+    float all = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+    const float extra = (float)((a.n_splits - 1) * a.batch);
+    n = lane < a.batch ? 1 + (int)(extra * (mine / all) * (1.f + 0x1p-20f)) : 0;
+    first = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int below = __shfl_up(first, d);
+        if (lane >= d) first += below;
+    }
+    first -= n;
+}
+// The place `at`; split = -1: nobody's.
+__device__ __forceinline__ Place place_at(const Args& a, int at) {
+    Place p;
+    if (!a.share) {
+        p.b = at / a.n_splits;
+        p.split = at - p.b * a.n_splits;
+        p.n = a.n_splits;
+        p.first = at - p.split;
+        return p;
+    }
+    const int lane = threadIdx.x & 63;
+    int n, first;
+    share_places(a, lane, n, first);
+    const uint64_t found = __ballot(at >= first && at < first + n);
+    const int who = found ? __ffsll((unsigned long long)found) - 1 : 0;
+    p.b = __builtin_amdgcn_readfirstlane(who);
+    p.n = __builtin_amdgcn_readlane(n, p.b);
+    p.first = __builtin_amdgcn_readlane(first, p.b);
+    p.split = found ? at - p.first : -1;
+    return p;
+}
+// The places of sequence b.
+__device__ __forceinline__ Place places_of(const Args& a, int b) {
+    Place p = {b, 0, a.n_splits, b * a.n_splits};
+    if (a.share) {
+        int n, first;
+        share_places(a, threadIdx.x & 63, n, first);
+        p.n = __builtin_amdgcn_readlane(n, b);
+        p.first = __builtin_amdgcn_readlane(first, b);
+    }
+    return p;
+}
+
 // Nodes that node i of sequence b sees.
 __device__ __forceinline__ uint64_t node_mask(const Args& a, int b, int i) {
     if (a.tree) return a.tree[(int64_t)b * a.tree_stride + i];
@@ -90,10 +151,19 @@ __device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, 
     return u;
 }
 
-// y = cap * tanh(y / cap).  Up to 0.35 by the series to x^11 (1.2e-8 relative; the exponential form cancels there), beyond by
-// 1 - 2 / (1 + e^2x), for which one branch asks on behalf of all N scores: most tiles have none.
-template <int N>
+// y = cap * tanh(y / cap) as cap - 2 cap / (1 + e^(2 y / cap)), off by up to 8 * 2^-24 of the cap.  A weight is then off by less than an eighth of
+// half a step of fp16 as long as the cap is at most kCapExp; larger caps and exact ones take the series to x^11 up to 0.35 (1.2e-8 relative),
+// where this form cancels, with one branch that asks on behalf of all N scores whether any is beyond.
+constexpr float kCapExp = 96.f;                // base 2: 8 * 2^-24 * 96 * ln 2 < 2^-14.9
+template <int N, bool EXACT>
 __device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_cap) {
+    const float turn = inv_cap * 2.8853900817779268f;
+    auto by_exp = [&](float v) { return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + exp2_raw(v * turn)), cap); };
+    if (!EXACT && cap <= kCapExp) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = by_exp(y[i]);
+        return;
+    }
     float most = 0.f, v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -108,12 +178,7 @@ __device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_c
     constexpr float kSeries = 0.35f;
     if (__builtin_amdgcn_ballot_w64(most > kSeries)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float x = fabsf(y[i] * inv_cap);
-            const float e = exp2_raw(x * -2.8853900817779268f);
-            const float h = cap * fmaf(-2.f * e, __builtin_amdgcn_rcpf(1.f + e), 1.f);
-            v[i] = x > kSeries ? copysignf(h, y[i]) : v[i];
-        }
+        for (int i = 0; i < N; ++i) v[i] = fabsf(y[i] * inv_cap) > kSeries ? by_exp(y[i]) : v[i];
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = v[i];
@@ -121,9 +186,9 @@ __device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_c
 
 // Scores (base 2) of one row for the tokens t0 + 16 (i / 4) + i % 4, i < N; -inf where a token is not seen.  `inner`: all of them are
 // seen, and are no nodes.
-template <int N>
+template <int N, bool EXACT>
 __device__ __forceinline__ void rule_scores(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, bool inner, int t0, float (&y)[N]) {
-    if (a.cap != 0.f) cap_scores<N>(y, a.cap, a.inv_cap);
+    if (a.cap != 0.f) cap_scores<N, EXACT>(y, a.cap, a.inv_cap);
     if (inner) {
         if (a.slopes) {
             const float far = (float)(u.pos - t0);

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i] * mul;
         }
-        rule_scores<8>(a, s, u, depth_s, false, t0 + 4 * group, y);
+        rule_scores<8, true>(a, s, u, depth_s, false, t0 + 4 * group, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(y[i] - ref) : 0.f;
     }

@@ -70,7 +70,8 @@ def scores(q, keys, scale, sizes, perm_k, rule):
             off = (D + 8) * U * (np.abs(qq) @ np.abs(k).T * abs(scale))
             if cap:
                 y = cap * np.tanh(y / cap)
-                off = off + 8 * U * np.abs(y)
+                # up to eight roundings of the result, or of the cap where the exponential form stands alone (16-bit I/O)
+            off = off + 8 * U * np.maximum(np.abs(y), cap if rule.get("by_exp") and cap <= 64 else 0)
             if slopes is not None:
                 bias = slopes[head] * np.abs(far)
                 y = y - bias

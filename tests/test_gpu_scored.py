@@ -35,6 +35,7 @@ def run_case(seed, B, H, G, n, S, bits, block, dtype, page=0, lens=None, perm=Fa
     scale = float(np.float32(scale))
     cap64 = float(np.float32(cap))
     rule["cap"] = cap64
+    rule["by_exp"] = dtype != F32
     lse = torch.full((B, n, H * G), 7.0, device="cuda") if with_lse else None
     lens_dev = None if lens is None else dev_i32(np.array(lens))
     args = dict(rule=dev, seq_len_dev=lens_dev, perm_k=dev_i32(pk), perm_v=dev_i32(pv), lse=lse, out=torch.full_like(q, float("nan")))
