@@ -71,27 +71,38 @@ __device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const b
     }
 }
 
-// Running maximum of one row over the tokens of a tile: the sums follow it.  Returns what the scores are taken relative to.
-__device__ __forceinline__ float follow(float top, float& m, float& l, f32x4 (&o)[8]) {
-    top = rows_max(top);
-    if (__builtin_amdgcn_ballot_w64(top > m)) {
-        const float now = fmaxf(m, top);
-        const float f = now > -INFINITY ? exp2_raw(m - now) : 1.f;
-        m = now;
-        l *= f;
+// Running maximum of one row over the tokens of a tile.  The sums are relative to a reference that scores may exceed by 2^kSlack before they
+// are rescaled: 16 rows have a new maximum nearly every tile otherwise, and 32 products each time (64 nodes over 8 x 8k tokens 166 -> KSLACK us).
+// Sums of values with exponent bytes up to kOrdinary have room for that (below 2^74, times 2^kSlack, times 2^30 tokens); from the first
+// larger byte on the reference is the maximum itself.
+constexpr float kSlack = 8.f;
+constexpr uint32_t kOrdinary = 200;
+struct Running {
+    float ref = -INFINITY, most = -INFINITY, sum = 0.f;
+};
+__device__ __forceinline__ float follow(float top, float slack, Running& x, f32x4 (&o)[8]) {
+    x.most = fmaxf(x.most, rows_max(top));
+    if (__builtin_amdgcn_ballot_w64(x.most > x.ref + slack)) {        // (the reference begins at minus infinity)
+        const float f = x.most > -INFINITY ? exp2_raw(x.ref - x.most) : 1.f;
+        x.ref = x.most;
+        x.sum *= f;
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[ct][i] *= f;
     }
-    return m > -INFINITY ? m : 0.f;
+    return x.ref > -INFINITY ? x.ref : 0.f;
+}
+template <int P, bool N16>
+__device__ __forceinline__ bool has_large(const Chunk<P, N16>& c) {
+    return c.e[0] > kOrdinary || (N16 && c.e[N16 ? 1 : 0] > kOrdinary);
 }
 // Eight scores of a row -> its probabilities as the operand of add_values, and their sum.
 template <int PL>
-__device__ __forceinline__ void probabilities(const float* y, float ref, float& l, bf16x8 (&p)[PL]) {
+__device__ __forceinline__ void probabilities(const float (&y)[8], float factor, float ref, float& l, bf16x8 (&p)[PL]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float w = exp2_raw(y[i] - ref);
+        const float w = exp2_raw(fmaf(y[i], factor, -ref));
         l += w;
         __bf16 lw[PL];
         limbs<PL>(w, lw);
@@ -120,15 +131,15 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
 // free when this is called.
 template <int P, int QL, int RW>
 __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int place, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
-                                       const f32x4 (&o)[8], float m, float l) {
+                                       const f32x4 (&o)[8], const Running& x) {
     const int tid = threadIdx.x, l16 = lane & 15, group = lane >> 4;
-    constexpr float up = (float)(1 << Decode<P>::kShift);
+    constexpr float up = (float)(1 << Decode<P>::kShift);       // (partial results keep the scale of the decoded values)
     float* const o_s = (float*)(smem + wave * kWaveLds);
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) *(f32x4*)(o_s + l16 * kOStride + 16 * ct + 4 * group) = o[ct];
-    const float sum = rows_sum(l);
+    const float sum = rows_sum(x.sum);
     if (group == 0) {
-        ml_s[wave][l16][0] = m;
+        ml_s[wave][l16][0] = x.ref;
         ml_s[wave][l16][1] = sum;
     }
     __syncthreads();
@@ -155,8 +166,8 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
                 a.part_ml[2 * at] = top;
                 a.part_ml[2 * at + 1] = den;
             }
-            *(f32x4*)(a.part_o + at * kD + p0) = f32x4{acc[0] * up, acc[1] * up, acc[2] * up, acc[3] * up};
-            *(f32x4*)(a.part_o + at * kD + p0 + 4) = f32x4{acc[4] * up, acc[5] * up, acc[6] * up, acc[7] * up};
+            *(f32x4*)(a.part_o + at * kD + p0) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+            *(f32x4*)(a.part_o + at * kD + p0 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
         } else {
             const int64_t at = out_row(a, b, kvh, r);
             const float by = den > 0.f ? up / den : 0.f;
@@ -218,7 +229,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 
     uint8_t* const v_s = smem + wave * kWaveLds;
     f32x4 o[1][8];
-    float m = -INFINITY, l = 0.f;
+    Running x;
+    float slack = kSlack;
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) o[0][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
@@ -256,25 +268,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][j], sc, 0, 0, 0);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i] * mul;
+            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i];
         }
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
+        if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) slack = 0.f;
         wave_fence();
-        rule_scores<8, QL == 3>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, y);
+        const float factor = rule_scores<8, QL == 3>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, mul, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
-        const float ref = follow(top, m, l, o[0]);
+        const float ref = follow(top * factor, slack, x, o[0]);
         bf16x8 p[1][PL];
-        probabilities<PL>(y, ref, l, p[0]);
+        probabilities<PL>(y, factor, ref, x.sum, p[0]);
         add_values<PL, 1>(v_s, lane, p, o);
         wave_fence();
     }
     __syncthreads();
-    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], m, l);
+    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x);
 }
 
 // More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
@@ -290,6 +303,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     __shared__ float ml_s[4][16][2];
     __shared__ int perm_s[kD];
     __shared__ int depth_s[64];
+    __shared__ int large_s[2];                               // a value byte above kOrdinary was decoded into this half
     static_assert(16 * RW * kQStride * 4 <= 2 * kTile && 4 * kWaveLds <= 2 * kTile, "the query rows and the sums fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
@@ -313,6 +327,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     int lo_least, lo_most;
     row_limits<HC>(u, lo_least, lo_most);
+    if (tid < 2) large_s[tid] = 0;
     if (lane == 0) ml_s[0][wave][0] = __int_as_float(lo_least);        // (as bits) tiles are the workgroup's, not the wavefront's
     __syncthreads();
 #pragma unroll
@@ -320,14 +335,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     lo_least = __builtin_amdgcn_readfirstlane(lo_least);
 
     f32x4 o[HC][8];
-    float m[HC], l[HC];
+    Running x[HC];
 #pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        m[c] = -INFINITY;
-        l[c] = 0.f;
+    for (int c = 0; c < HC; ++c)
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct) o[c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
     const auto tiles = tiles_of<kWideTokens>(s, lo_least);
     const int last16 = (s.len - 1) & ~15;
@@ -342,21 +354,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_raw);
     };
     auto key_at = [](int row, int piece) { return row * 256 + ((piece ^ (row & 15)) * 16); };
-    auto decode = [&](uint8_t* tile) {
+    auto decode = [&](int half) {
+        uint8_t* const tile = smem + half * kTile;
         const int row = 16 * wave + l16;
 #pragma unroll
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + key_at(row, 4 * group + j)) = eight<P, N16>(k_raw, j);
 #pragma unroll
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(v_raw, j);
+        if (__builtin_amdgcn_ballot_w64(has_large(v_raw)) && lane == 0) large_s[half] = 1;
     };
     request(split);
-    if (split < tiles.count) decode(smem);
+    if (split < tiles.count) decode(0);
     request(split + n_splits);
     int half = 0;
+    float slack = kSlack;
     for (int v = split; v < tiles.count; v += n_splits, half ^= 1) {
         __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
-        if (v + n_splits < tiles.count) decode(smem + (half ^ 1) * kTile);
+        if (large_s[half]) slack = 0.f;
+        if (v + n_splits < tiles.count) decode(half ^ 1);
         request(v + 2 * n_splits);
         // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
 #pragma unroll 1
@@ -379,18 +395,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int c = 0; c < HC; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[c][4 * ts + i] = sc[c][i] * mul;
+                    for (int i = 0; i < 4; ++i) y[c][4 * ts + i] = sc[c][i];
             }
             const bool inner = t0 >= lo_most && t0 + 32 <= s.base;
             bf16x8 p[HC][PL];
 #pragma unroll
             for (int c = 0; c < HC; ++c) {
                 float top = -INFINITY;
-                rule_scores<8, QL == 3>(a, s, u[c], depth_s, inner, t0 + 4 * group, y[c]);
+                const float factor = rule_scores<8, QL == 3>(a, s, u[c], depth_s, inner, t0 + 4 * group, mul, y[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, y[c][i]);
-                const float ref = follow(top, m[c], l[c], o[c]);
-                probabilities<PL>(y[c], ref, l[c], p[c]);
+                const float ref = follow(top * factor, slack, x[c], o[c]);
+                probabilities<PL>(y[c], factor, ref, x[c].sum, p[c]);
             }
             add_values<PL, HC>(tile + kPlane + row * 256, lane, p, o);
         }
@@ -398,7 +414,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int c = 0; c < HC; ++c) {
         __syncthreads();
-        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, blockIdx.x, smem, ml_s, wave, lane, o[c], m[c], l[c]);
+        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
     }
 }
 
@@ -464,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
             acc.y = fmaf(f, x[3], acc.y);
         }
     }
-    const float by = den > 0.f ? 1.f / den : 0.f;
+    const float by = den > 0.f ? (float)(1 << Decode<P>::kShift) / den : 0.f;
     const int64_t at = out_row(a, b, kvh, r);
     store_out<QL>(a, at * kD + c0, acc.x * by);
     store_out<QL>(a, at * kD + c1, acc.y * by);

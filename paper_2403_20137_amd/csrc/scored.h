@@ -66,7 +66,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
 
 // Which part of which sequence a place takes: part `split` of `n`, the places of the sequence begin at `first`.  Equal parts
 // (n_splits each), or shared out by what the sequences have to read (up to 64 of them, a lane each): one each, the others in
-// proportion.  (Rounded down, so that all fit: the sum of rounded-down shares is at most what there is to share.)
+// proportion, rounded down, what is left by the largest remainders.
 struct Place { int b, split, n, first; };
 __device__ __forceinline__ int tokens_read(const Args& a, int b) {        // about: documents are not looked at
     int len = min(max(a.seq_len[b], 0), a.max_len);
@@ -82,7 +82,19 @@ __device__ __forceinline__ void share_places(const Args& a, int lane, int& n, in
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
     const float extra = (float)((a.n_splits - 1) * a.batch);
-    n = lane < a.batch ? 1 + (int)(extra * (mine / all) * (1.f + 0x1p-20f)) : 0;
+    const float share = extra * (mine / all) * (1.f + 0x1p-20f);         // (a whole number stays one)
+    n = lane < a.batch ? 1 + (int)share : 0;
+    int left = n;                        // the sum of rounded-down shares is at most what there is to share
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) left += __shfl_xor(left, d);
+    left = a.n_splits * a.batch - left;
+    const float rest = share - floorf(share);
+    int before = 0;
+    for (int j = 0; j < a.batch; ++j) {
+        const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(rest), j));
+        before += other > rest || (other == rest && j < lane);
+    }
+    if (lane < a.batch && before < left) ++n;
     first = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -156,14 +168,16 @@ __device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, 
 // where this form cancels, with one branch that asks on behalf of all N scores whether any is beyond.
 constexpr float kCapExp = 96.f;                // base 2: 8 * 2^-24 * 96 * ln 2 < 2^-14.9
 template <int N, bool EXACT>
-__device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_cap) {
+__device__ __forceinline__ void cap_scores(float (&y)[N], float mul, float cap, float inv_cap) {
+    auto by_exp = [&](float v, float turn) { return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + exp2_raw(v * turn)), cap); };
     const float turn = inv_cap * 2.8853900817779268f;
-    auto by_exp = [&](float v) { return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + exp2_raw(v * turn)), cap); };
     if (!EXACT && cap <= kCapExp) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) y[i] = by_exp(y[i]);
+        for (int i = 0; i < N; ++i) y[i] = by_exp(y[i], mul * turn);
         return;
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] *= mul;
     float most = 0.f, v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -178,24 +192,34 @@ __device__ __forceinline__ void cap_scores(float (&y)[N], float cap, float inv_c
     constexpr float kSeries = 0.35f;
     if (__builtin_amdgcn_ballot_w64(most > kSeries)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = fabsf(y[i] * inv_cap) > kSeries ? by_exp(y[i]) : v[i];
+        for (int i = 0; i < N; ++i) v[i] = fabsf(y[i] * inv_cap) > kSeries ? by_exp(y[i], turn) : v[i];
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = v[i];
 }
 
-// Scores (base 2) of one row for the tokens t0 + 16 (i / 4) + i % 4, i < N; -inf where a token is not seen.  `inner`: all of them are
-// seen, and are no nodes.
+// Scores (base 2) of one row for the tokens t0 + 16 (i / 4) + i % 4, i < N, from the products of query and keys, which times `mul` are the
+// plain scores; -inf where a token is not seen.  `inner`: all of them are seen, and are no nodes.  Returns what they are still to
+// be multiplied with: 1, or a positive `mul` that nothing has to come before, which costs nothing in the exponent's multiply-add.
 template <int N, bool EXACT>
-__device__ __forceinline__ void rule_scores(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, bool inner, int t0, float (&y)[N]) {
-    if (a.cap != 0.f) cap_scores<N, EXACT>(y, a.cap, a.inv_cap);
+__device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, bool inner, int t0, float mul,
+                                             float (&y)[N]) {
+    float factor = 1.f;
+    if (a.cap != 0.f) {
+        cap_scores<N, EXACT>(y, mul, a.cap, a.inv_cap);
+    } else if (a.slopes || !(mul > 0.f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] *= mul;
+    } else {
+        factor = mul;
+    }
     if (inner) {
         if (a.slopes) {
             const float far = (float)(u.pos - t0);
 #pragma unroll
             for (int i = 0; i < N; ++i) y[i] = fmaf(-u.slope, far - (float)(16 * (i >> 2) + (i & 3)), y[i]);
         }
-        return;
+        return factor;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -210,6 +234,7 @@ __device__ __forceinline__ void rule_scores(const Args& a, const Seq& s, const R
         if (a.slopes) y[i] = fmaf(-u.slope, fabsf((float)far), y[i]);
         y[i] = seen ? y[i] : -INFINITY;
     }
+    return factor;
 }
 
 // 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).

@@ -79,11 +79,11 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
 #pragma unroll
                 for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st][j], q[i][j], sc, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i] * mul;
+            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i];
         }
-        rule_scores<8, true>(a, s, u, depth_s, false, t0 + 4 * group, y);
+        const float factor = rule_scores<8, true>(a, s, u, depth_s, false, t0 + 4 * group, mul, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(y[i] - ref) : 0.f;
+        for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(fmaf(y[i], factor, -ref)) : 0.f;
     }
     if (!some) return;
     // acc[4 st + i] of the 16 lanes of a group: token t0 + 16 st + 4 group + i
