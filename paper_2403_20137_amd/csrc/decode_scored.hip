@@ -71,17 +71,20 @@ __device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const b
     }
 }
 
-// Running maximum of one row over the tokens of a tile.  The sums are relative to a reference that scores may exceed by 2^kSlack before they
-// are rescaled: 16 rows have a new maximum nearly every tile otherwise, and 32 products each time (64 nodes over 8 x 8k tokens 166 -> KSLACK us).
-// Sums of values with exponent bytes up to kOrdinary have room for that (below 2^74, times 2^kSlack, times 2^30 tokens); from the first
-// larger byte on the reference is the maximum itself.
+// Running maximum of one row.  The sums are relative to a reference that scores may exceed by 2^kSlack before they are rescaled: 16 rows
+// have a new maximum nearly every tile otherwise, and 32 products each time.  Sums of values with exponent bytes up to kOrdinary have
+// room for that (below 2^74, times 2^kSlack, times 2^30 tokens); from the first larger byte on the reference is the maximum itself.
 constexpr float kSlack = 8.f;
 constexpr uint32_t kOrdinary = 200;
 struct Running {
     float ref = -INFINITY, most = -INFINITY, sum = 0.f;
 };
-__device__ __forceinline__ float follow(float top, float slack, Running& x, f32x4 (&o)[8]) {
-    x.most = fmaxf(x.most, rows_max(top));
+// Takes eight scores (y times factor) into account; returns what they are taken relative to.
+__device__ __forceinline__ float follow(const float (&y)[8], float factor, float slack, Running& x, f32x4 (&o)[8]) {
+    float top = y[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
+    x.most = fmaxf(x.most, rows_max(top * factor));
     if (__builtin_amdgcn_ballot_w64(x.most > x.ref + slack)) {        // (the reference begins at minus infinity)
         const float f = x.most > -INFINITY ? exp2_raw(x.ref - x.most) : 1.f;
         x.ref = x.most;
@@ -93,22 +96,43 @@ __device__ __forceinline__ float follow(float top, float slack, Running& x, f32x
     }
     return x.ref > -INFINITY ? x.ref : 0.f;
 }
-template <int P, bool N16>
-__device__ __forceinline__ bool has_large(const Chunk<P, N16>& c) {
-    return c.e[0] > kOrdinary || (N16 && c.e[N16 ? 1 : 0] > kOrdinary);
-}
 // Eight scores of a row -> its probabilities as the operand of add_values, and their sum.
 template <int PL>
-__device__ __forceinline__ void probabilities(const float (&y)[8], float factor, float ref, float& l, bf16x8 (&p)[PL]) {
+__device__ __forceinline__ void probabilities(const float (&y)[8], float factor, float base, float& sum, bf16x8 (&p)[PL]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float w = exp2_raw(fmaf(y[i], factor, -ref));
-        l += w;
+        const float w = exp2_raw(fmaf(y[i], factor, -base));
+        sum += w;
         __bf16 lw[PL];
         limbs<PL>(w, lw);
         if (PL == 2) lw[1] = (__bf16)(w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));     // rounded, not cut
 #pragma unroll
         for (int x = 0; x < PL; ++x) p[x][i] = lw[x];
+    }
+}
+template <int P, bool N16>
+__device__ __forceinline__ bool has_large(const Chunk<P, N16>& c) { return max(c.e[0], c.e[N16 ? 1 : 0]) > kOrdinary; }
+
+// Scores of 32 tokens for HC times 16 rows: products of the keys of two stages of 16 tokens, key(stage, step) an operand, with the queries.
+template <int QL, int HC, class Key>
+__device__ __forceinline__ void products(Key&& key, const bf16x8 (&q)[HC][QL][4], float (&y)[HC][8]) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        f32x4 sc[HC];
+#pragma unroll
+        for (int c = 0; c < HC; ++c) sc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bf16x8 k = key(st, j);
+#pragma unroll
+            for (int c = 0; c < HC; ++c)
+#pragma unroll
+                for (int i = 0; i < QL; ++i) sc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][i][j], sc[c], 0, 0, 0);
+        }
+#pragma unroll
+        for (int c = 0; c < HC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[c][4 * st + i] = sc[c][i];
     }
 }
 
@@ -126,6 +150,16 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
     return ((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G);
 }
 
+// Partial results of a wavefront's own 16 rows from r0 on.
+__device__ __forceinline__ void store_partial(const Args& a, int kvh, int r0, int place, int lane, const f32x4 (&o)[8], const Running& x) {
+    const int l16 = lane & 15, group = lane >> 4, r = r0 + l16;
+    const float sum = rows_sum(x.sum);
+    if (r >= a.M) return;
+    const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) *(f32x4*)(a.part_o + at * kD + 16 * ct + 4 * group) = o[ct];
+    if (group == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(x.ref, sum);
+}
 // The sums of a workgroup's wavefronts for 16 * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
 // 16 (w % RW) ..) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
 // free when this is called.
@@ -162,10 +196,7 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
         }
         if (a.n_splits > 1) {
             const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
-            if (p0 == 0) {
-                a.part_ml[2 * at] = top;
-                a.part_ml[2 * at + 1] = den;
-            }
+            if (p0 == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(top, den);
             *(f32x4*)(a.part_o + at * kD + p0) = f32x4{acc[0], acc[1], acc[2], acc[3]};
             *(f32x4*)(a.part_o + at * kD + p0 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
         } else {
@@ -182,26 +213,8 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
     }
 }
 
-// The rows of the workgroup's heads that matter to what it reads: the first token that some row sees, and from where on all do.
-template <int HC>
-__device__ __forceinline__ void row_limits(const RowRule (&u)[HC], int& least, int& most) {
-    most = INT32_MIN;
-    least = INT32_MAX;
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        most = max(most, u[c].lo);
-        least = min(least, u[c].lo);
-    }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        most = max(most, __shfl_xor(most, d));
-        least = min(least, __shfl_xor(least, d));
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
-    least = __builtin_amdgcn_readfirstlane(least);
-}
-
-// Up to 16 rows.  grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL limbs of the query.
+// Up to 16 rows: every wavefront has all of them and takes 32 tokens of a tile of 128 for itself.
+// grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL bf16 numbers of a query.
 template <int P, bool N16, int QL>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
@@ -209,31 +222,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     __shared__ float ml_s[4][16][2];
     __shared__ int perm_s[kD];
     __shared__ int depth_s[64];
+    __shared__ RowRule rule_s[16];
     static_assert(16 * kQStride * 4 <= 4 * kWaveLds, "the query rows fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
     const Place place = place_at(a, blockIdx.x);
     if (place.split < 0) return;
-    const int b = place.b, kvh = blockIdx.y, split = place.split, n_splits = place.n;
+    const int b = place.b, kvh = blockIdx.y, n_splits = place.n;
+    QueryRows<QL, 16> rows;
+    rows.request(a, b, kvh, 0);
     const Seq s = sequence(a, b);
-
-    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    stage_queries<QL, 16>(a, b, kvh, 0, (float*)smem, perm_s);
-    const RowRule u[1] = {row_rule(a, s, b, kvh, l16)};
     int lo_least, lo_most;
-    row_limits<1>(u, lo_least, lo_most);
-    __syncthreads();
-    bf16x8 q[QL][4];
-    query_operand<P, QL>((const float*)smem, perm_s, l16, group, q);
-    __syncthreads();                                         // the queries give way to the values
-
-    uint8_t* const v_s = smem + wave * kWaveLds;
-    f32x4 o[1][8];
-    Running x;
-    float slack = kSlack;
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) o[0][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    row_limits(a, s, b, 0, 16, lo_least, lo_most);
     const auto tiles = tiles_of<kTileTokens>(s, lo_least);
     const int last16 = (s.len - 1) & ~15;
     Chunk<P, N16> k_next[2], v_next[2];
@@ -249,27 +249,31 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_next[st]);
         }
     };
-    request(split);
-    for (int v = split; v < tiles.count; v += n_splits) {
+    request(place.split);
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    rows.put(a, 0, (float*)smem, perm_s);
+    if (tid < 16) rule_s[tid] = row_rule(a, s, b, kvh, tid);
+    __syncthreads();
+    bf16x8 q[1][QL][4];
+    query_operand<P, QL>((const float*)smem, perm_s, l16, group, q[0]);
+    __syncthreads();                                         // the queries give way to the values
+
+    uint8_t* const v_s = smem + wave * kWaveLds;
+    f32x4 o[1][8];
+    Running x[1];
+    float slack = kSlack;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) o[0][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    for (int v = place.split; v < tiles.count; v += n_splits) {
         const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
         if (t0 >= s.len) break;                              // the wavefront's part of the last tile is empty
         Chunk<P, N16> kc[2], vc[2];
 #pragma unroll
         for (int st = 0; st < 2; ++st) { kc[st] = k_next[st]; vc[st] = v_next[st]; }
         request(v + n_splits);
-        float y[8], top = -INFINITY;
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 k = __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j));
-#pragma unroll
-                for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][j], sc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i];
-        }
+        float y[1][8];
+        products<QL, 1>([&](int st, int j) { return __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j)); }, q, y);
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -277,17 +281,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
         if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) slack = 0.f;
         wave_fence();
-        const float factor = rule_scores<8, QL == 3>(a, s, u[0], depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, mul, y);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i]);
-        const float ref = follow(top * factor, slack, x, o[0]);
+        const float factor = rule_scores<8, QL == 3>(a, s, rule_s + l16, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, mul, y[0]);
+        const float base = follow(y[0], factor, slack, x[0], o[0]);
         bf16x8 p[1][PL];
-        probabilities<PL>(y, factor, ref, x.sum, p[0]);
+        probabilities<PL>(y[0], factor, base, x[0].sum, p[0]);
         add_values<PL, 1>(v_s, lane, p, o);
         wave_fence();
     }
     __syncthreads();
-    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x);
+    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
 }
 
 // More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
@@ -303,44 +305,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     __shared__ float ml_s[4][16][2];
     __shared__ int perm_s[kD];
     __shared__ int depth_s[64];
+    __shared__ RowRule rule_s[16 * RW * HC];
     __shared__ int large_s[2];                               // a value byte above kOrdinary was decoded into this half
     static_assert(16 * RW * kQStride * 4 <= 2 * kTile && 4 * kWaveLds <= 2 * kTile, "the query rows and the sums fit");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
     const Place place = place_at(a, blockIdx.x);
     if (place.split < 0) return;
-    const int b = place.b, split = place.split, n_splits = place.n;
+    const int b = place.b, n_splits = place.n;
     const int kvh = blockIdx.y / a.row_tiles, r0 = (blockIdx.y % a.row_tiles) * (16 * HC * RW);
     const int rw = wave % RW, part = wave / RW;              // its rows; its part of a tile's tokens
+    QueryRows<QL, 16 * RW> rows[HC];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) rows[c].request(a, b, kvh, r0 + 16 * RW * c);
     const Seq s = sequence(a, b);
-
-    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    RowRule u[HC];
-    bf16x8 q[HC][QL][4];
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        u[c] = row_rule(a, s, b, kvh, r0 + 16 * (RW * c + rw) + l16);
-        if (c > 0) __syncthreads();
-        stage_queries<QL, 16 * RW>(a, b, kvh, r0 + 16 * RW * c, (float*)smem, perm_s);
-        __syncthreads();
-        query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[c]);
-    }
     int lo_least, lo_most;
-    row_limits<HC>(u, lo_least, lo_most);
-    if (tid < 2) large_s[tid] = 0;
-    if (lane == 0) ml_s[0][wave][0] = __int_as_float(lo_least);        // (as bits) tiles are the workgroup's, not the wavefront's
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 4; ++w) lo_least = min(lo_least, __float_as_int(ml_s[0][w][0]));
-    lo_least = __builtin_amdgcn_readfirstlane(lo_least);
-
-    f32x4 o[HC][8];
-    Running x[HC];
-#pragma unroll
-    for (int c = 0; c < HC; ++c)
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) o[c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    row_limits(a, s, b, r0, 16 * RW * HC, lo_least, lo_most);
     const auto tiles = tiles_of<kWideTokens>(s, lo_least);
     const int last16 = (s.len - 1) & ~15;
     // a thread decodes 32 channels of one token, keys and values: wavefront w tokens 16 w ..
@@ -353,6 +333,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_raw);
         load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_raw);
     };
+    request(place.split);
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    if (tid < 2) large_s[tid] = 0;
+    for (int i = tid; i < 16 * RW * HC; i += kThreads) rule_s[i] = row_rule(a, s, b, kvh, r0 + i);
+    bf16x8 q[HC][QL][4];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) {
+        if (c > 0) __syncthreads();
+        rows[c].put(a, r0 + 16 * RW * c, (float*)smem, perm_s);
+        __syncthreads();
+        query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[c]);
+    }
+    __syncthreads();                                         // the queries give way to keys and values
+
+    f32x4 o[HC][8];
+    Running x[HC];
+#pragma unroll
+    for (int c = 0; c < HC; ++c)
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) o[c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
     auto key_at = [](int row, int piece) { return row * 256 + ((piece ^ (row & 15)) * 16); };
     auto decode = [&](int half) {
         uint8_t* const tile = smem + half * kTile;
@@ -363,58 +364,42 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(v_raw, j);
         if (__builtin_amdgcn_ballot_w64(has_large(v_raw)) && lane == 0) large_s[half] = 1;
     };
-    request(split);
-    if (split < tiles.count) decode(0);
-    request(split + n_splits);
+    if (place.split < tiles.count) decode(0);
+    request(place.split + n_splits);
     int half = 0;
     float slack = kSlack;
-    for (int v = split; v < tiles.count; v += n_splits, half ^= 1) {
+    for (int v = place.split; v < tiles.count; v += n_splits, half ^= 1) {
         __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
-        if (large_s[half]) slack = 0.f;
         if (v + n_splits < tiles.count) decode(half ^ 1);
         request(v + 2 * n_splits);
+        if (large_s[half]) slack = 0.f;
         // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
 #pragma unroll 1
         for (int ks = 0; ks < KS; ++ks) {
             const int row = 32 * (KS * part + ks), t0 = tiles.at(v) * kWideTokens + row;
             float y[HC][8];
-#pragma unroll
-            for (int ts = 0; ts < 2; ++ts) {
-                f32x4 sc[HC];
-#pragma unroll
-                for (int c = 0; c < HC; ++c) sc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 k = *(const bf16x8*)(tile + key_at(row + 16 * ts + l16, 4 * group + j));
-#pragma unroll
-                    for (int c = 0; c < HC; ++c)
-#pragma unroll
-                        for (int i = 0; i < QL; ++i) sc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][i][j], sc[c], 0, 0, 0);
-                }
-#pragma unroll
-                for (int c = 0; c < HC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[c][4 * ts + i] = sc[c][i];
-            }
+            products<QL, HC>([&](int st, int j) { return *(const bf16x8*)(tile + key_at(row + 16 * st + l16, 4 * group + j)); }, q, y);
             const bool inner = t0 >= lo_most && t0 + 32 <= s.base;
             bf16x8 p[HC][PL];
 #pragma unroll
             for (int c = 0; c < HC; ++c) {
-                float top = -INFINITY;
-                const float factor = rule_scores<8, QL == 3>(a, s, u[c], depth_s, inner, t0 + 4 * group, mul, y[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, y[c][i]);
-                const float ref = follow(top * factor, slack, x[c], o[c]);
-                probabilities<PL>(y[c], factor, ref, x[c].sum, p[c]);
+                const float factor = rule_scores<8, QL == 3>(a, s, rule_s + 16 * (RW * c + rw) + l16, depth_s, inner, t0 + 4 * group, mul, y[c]);
+                const float base = follow(y[c], factor, slack, x[c], o[c]);
+                probabilities<PL>(y[c], factor, base, x[c].sum, p[c]);
             }
             add_values<PL, HC>(tile + kPlane + row * 256, lane, p, o);
         }
     }
 #pragma unroll
     for (int c = 0; c < HC; ++c) {
-        __syncthreads();
-        if (r0 + 16 * RW * c < a.M) finish<P, QL, RW>(a, b, kvh, r0 + 16 * RW * c, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
+        const int rc = r0 + 16 * RW * c;
+        if (RW == 4 && a.n_splits > 1) {                     // nothing to join
+            store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[c], x[c]);
+        } else {
+            __syncthreads();
+            if (rc < a.M) finish<P, QL, RW>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
+        }
     }
 }
 
@@ -487,23 +472,28 @@ __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
     if (lane == 0 && a.lse) a.lse[at] = natural_lse(top, den);
 }
 
-// Rows of a workgroup: 16 in scored_split, 16 * rw * hc in scored_split_wide; splits: enough workgroups for the compute units, and no
-// more than there are tiles.
+// Rows of a workgroup: 16 in scored_split (rw = 1), 16 * rw * hc in scored_split_wide; splits: enough workgroups for the compute units, and
+// no more than there are tiles.
 struct Plan { int32_t hc, rw, row_tiles, n_splits; };
 
 template <int P, bool N16, int QL>
 void launch_split(const Args& a, const Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)(a.H_kv * a.row_tiles));
+    constexpr int kTwo = QL == 1 ? 2 : 1;                    // fp16 and fp32 have no registers for two, and are not planned with them
     if (p.rw == 1) scored_split<P, N16, QL><<<grid, kThreads, 0, s>>>(a);
     else if (p.rw == 2) scored_split_wide<P, N16, QL, 1, 2><<<grid, kThreads, 0, s>>>(a);
-    else if (QL == 3 || p.hc == 1) scored_split_wide<P, N16, QL, 1, 4><<<grid, kThreads, 0, s>>>(a);
-    else scored_split_wide<P, N16, QL, QL == 3 ? 1 : 2, 4><<<grid, kThreads, 0, s>>>(a);
+    else if (p.hc == 1) scored_split_wide<P, N16, QL, 1, 4><<<grid, kThreads, 0, s>>>(a);
+    else scored_split_wide<P, N16, QL, kTwo, 4><<<grid, kThreads, 0, s>>>(a);
 }
-template <int P, bool N16>
+template <int P>
 void launch_split(const Args& a, int dt, const Plan& p, hipStream_t s) {
-    if (dt == KVBFP_F32) launch_split<P, N16, 3>(a, p, s);
-    else if (dt == KVBFP_F16) launch_split<P, N16, 2>(a, p, s);
-    else launch_split<P, N16, 1>(a, p, s);
+    const bool n16 = a.log2_block == 4;
+    if (dt == KVBFP_F32 && n16) launch_split<P, true, 3>(a, p, s);
+    else if (dt == KVBFP_F32) launch_split<P, false, 3>(a, p, s);
+    else if (dt == KVBFP_F16 && n16) launch_split<P, true, 2>(a, p, s);
+    else if (dt == KVBFP_F16) launch_split<P, false, 2>(a, p, s);
+    else if (n16) launch_split<P, true, 1>(a, p, s);
+    else launch_split<P, false, 1>(a, p, s);
 }
 
 // Few rows with many splits: four wavefronts for each.
@@ -520,25 +510,21 @@ void launch_combine(const Args& a, int dt, hipStream_t s) {
     else launch_combine<P, 1>(a, s);
 }
 
-Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
+// The splits, and with them the workspace, do not depend on the type.
+int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
+    const int64_t of_wg = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads * ((rows + of_wg - 1) / of_wg);
+    const int64_t tile = rows > 16 ? kWideTokens : kTileTokens, tiles = (max_len + tile - 1) / tile;
+    const int64_t wanted = rows <= 16 ? 768 : 512;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (wanted + units - 1) / units));
+}
+Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
     Plan p;
-    p.hc = rows > 64 ? 2 : 1;
+    p.hc = rows > 64 && dtype == KVBFP_BF16 ? 2 : 1;
     p.rw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t of_wg = 16 * p.hc * p.rw;
     p.row_tiles = (int32_t)((rows + of_wg - 1) / of_wg);
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads * p.row_tiles;
-    const int64_t tile = p.rw == 1 ? kTileTokens : kWideTokens, tiles = (max_len + tile - 1) / tile;
-    const int64_t wanted = p.rw == 1 ? 768 : 512;
-    p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (wanted + units - 1) / units));
-    return p;
-}
-// The splits, and with them the workspace, do not depend on the type; fp32 I/O has 64 rows a workgroup at most.
-Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
-    Plan p = plan(L, rows, max_len);
-    if (dtype == KVBFP_F32 && p.hc == 2) {
-        p.hc = 1;
-        p.row_tiles = (int32_t)((rows + 63) / 64);
-    }
+    p.n_splits = splits_of(L, rows, max_len);
     return p;
 }
 
@@ -638,14 +624,8 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
         a.part_ml = a.part_o + (size_t)a.batch * a.H_kv * a.M * a.n_splits * kD;
     }
     hipStream_t s = (hipStream_t)hip_stream;
-    const bool n16 = logical.block == 16;
-    if (logical.mant_bits == 4) {
-        if (n16) launch_split<4, true>(a, (int)dtype, p, s);
-        else launch_split<4, false>(a, (int)dtype, p, s);
-    } else {
-        if (n16) launch_split<8, true>(a, (int)dtype, p, s);
-        else launch_split<8, false>(a, (int)dtype, p, s);
-    }
+    if (logical.mant_bits == 4) launch_split<4>(a, (int)dtype, p, s);
+    else launch_split<8>(a, (int)dtype, p, s);
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && a.n_splits > 1) {
         if (logical.mant_bits == 4) launch_combine<4>(a, (int)dtype, s);
@@ -666,7 +646,7 @@ size_t kvbfp_scored_workspace_bytes(const kvbfp_layout* L, int32_t n_q_heads, in
         return 0;
     }
     const int64_t rows = (int64_t)(n_q_heads / L->n_kv_heads) * n_q_tokens;
-    return std::max<size_t>(partial_bytes(L, rows, plan(L, rows, max_len).n_splits), 256);
+    return std::max<size_t>(partial_bytes(L, rows, splits_of(L, rows, max_len)), 256);
 }
 
 size_t kvbfp_scored_workspace_bytes_paged(const kvbfp_layout* pool, int64_t table_stride, int32_t batch, int32_t n_q_heads,

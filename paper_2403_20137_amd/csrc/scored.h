@@ -151,6 +151,29 @@ struct RowRule {
     int32_t first, pos;        // nodes: from `first` on, nearer than the window
     float slope;               // base 2
 };
+// The tokens before the nodes that rows r0 .. r0 + count see (count <= 128): none before `least`, all of them from `most` on.  By
+// every wavefront for itself.
+__device__ __forceinline__ void row_limits(const Args& a, const Seq& s, int b, int r0, int count, int& least, int& most) {
+    least = most = 0;
+    if (!a.first && !a.window) return;
+    least = INT32_MAX;
+    most = INT32_MIN;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = min(r0 + min((int)(threadIdx.x & 63) + 64 * h, count - 1), a.M - 1) / a.G;
+        const int first = a.first ? a.first[(int64_t)b * a.n_tok + i] : 0;
+        const int lo = a.window ? max(first, s.base + node_depth(node_mask(a, b, i), i) - a.window + 1) : first;
+        least = min(least, lo);
+        most = max(most, lo);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        least = min(least, __shfl_xor(least, d));
+        most = max(most, __shfl_xor(most, d));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+}
 __device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, int kvh, int r) {
     r = min(r, a.M - 1);
     const int i = r / a.G, head = kvh * a.G + r - i * a.G;
@@ -200,9 +223,10 @@ __device__ __forceinline__ void cap_scores(float (&y)[N], float mul, float cap, 
 
 // Scores (base 2) of one row for the tokens t0 + 16 (i / 4) + i % 4, i < N, from the products of query and keys, which times `mul` are the
 // plain scores; -inf where a token is not seen.  `inner`: all of them are seen, and are no nodes.  Returns what they are still to
-// be multiplied with: 1, or a positive `mul` that nothing has to come before, which costs nothing in the exponent's multiply-add.
+// be multiplied with: 1, or a positive `mul` that nothing has to come before, which costs nothing in the exponent's multiply-add.  The rule
+// lies in LDS: few tiles ask for it.
 template <int N, bool EXACT>
-__device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const RowRule& u, const int* depth_s, bool inner, int t0, float mul,
+__device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t0, float mul,
                                              float (&y)[N]) {
     float factor = 1.f;
     if (a.cap != 0.f) {
@@ -215,12 +239,13 @@ __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const 
     }
     if (inner) {
         if (a.slopes) {
-            const float far = (float)(u.pos - t0);
+            const float far = (float)(rule_s->pos - t0), slope = rule_s->slope;
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = fmaf(-u.slope, far - (float)(16 * (i >> 2) + (i & 3)), y[i]);
+            for (int i = 0; i < N; ++i) y[i] = fmaf(-slope, far - (float)(16 * (i >> 2) + (i & 3)), y[i]);
         }
         return factor;
     }
+    const RowRule u = *rule_s;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int t = t0 + 16 * (i >> 2) + (i & 3), node = t - s.base;
@@ -237,7 +262,7 @@ __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const 
     return factor;
 }
 
-// 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).
+// 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).  N16: blocks of 16, two in a chunk.
 template <int P, bool N16>
 struct Chunk {
     u32x4 m[P / 4];
@@ -338,34 +363,49 @@ struct Io<2> { typedef _Float16 T; };
 template <>
 struct Io<3> { typedef float T; };
 
-// Puts ROWS query rows from r0 on into q_s[ROWS][kQStride] as fp32, in the query's own channel order (zeros behind the last row of the
-// kv-head), and the permutation into perm_s[kD].  Called by the whole workgroup of 256; the caller puts a barrier behind it.
+// ROWS query rows from r0 on (zeros behind the last row of the kv-head) on their way to q_s[ROWS][kQStride] as fp32, in the query's own channel
+// order, and the permutation to perm_s[kD].  Called by the whole workgroup of 256; the caller puts a barrier behind put().
 constexpr int kQStride = kD + 4;
 template <int QL, int ROWS>
-__device__ __forceinline__ void stage_queries(const Args& a, int b, int kvh, int r0, float* q_s, int* perm_s) {
+struct QueryRows {
     typedef typename Io<QL>::T T;
     typedef T Tx8 __attribute__((ext_vector_type(8)));
-    const int tid = threadIdx.x;
-    if (tid < kD) perm_s[tid] = a.perm_k ? a.perm_k[kvh * kD + tid] & (kD - 1) : tid;      // masked: stays inside the row
-    const bool vec = ((uintptr_t)a.q & 15u) == 0;
+    Tx8 x[ROWS / 16];
+    int perm;
+    __device__ __forceinline__ void request(const Args& a, int b, int kvh, int r0) {
+        const int tid = threadIdx.x;
+        perm = a.perm_k ? a.perm_k[kvh * kD + (tid & (kD - 1))] & (kD - 1) : tid & (kD - 1);      // masked: stays inside the row
+        const bool vec = ((uintptr_t)a.q & 15u) == 0;
 #pragma unroll
-    for (int p = 0; p < ROWS / 16; ++p) {
-        const int row = (tid >> 4) + 16 * p, c = (tid & 15) * 8, r = r0 + row;
-        Tx8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (r < a.M) {
-            const int tok = r / a.G;
-            const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
+        for (int p = 0; p < ROWS / 16; ++p) {
+            const int c = (tid & 15) * 8, r = r0 + (tid >> 4) + 16 * p, rc = min(r, a.M - 1), tok = rc / a.G;
+            const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (rc - tok * a.G)) * kD + c;
             if (vec) {
-                x = *(const Tx8*)src;
+                x[p] = *(const Tx8*)src;
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = src[k];
+                for (int k = 0; k < 8; ++k) x[p][k] = src[k];
             }
         }
-        *(f32x4*)(q_s + row * kQStride + c) = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
-        *(f32x4*)(q_s + row * kQStride + c + 4) = f32x4{(float)x[4], (float)x[5], (float)x[6], (float)x[7]};
     }
-}
+    __device__ __forceinline__ void put(const Args& a, int r0, float* q_s, int* perm_s) const {
+        const int tid = threadIdx.x;
+        if (tid < kD) perm_s[tid] = perm;
+#pragma unroll
+        for (int p = 0; p < ROWS / 16; ++p) {
+            const int row = (tid >> 4) + 16 * p;
+            float* const to = q_s + row * kQStride + (tid & 15) * 8;
+            const float there = r0 + row < a.M ? 1.f : 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 v;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = there != 0.f ? (float)x[p][4 * h + k] : 0.f;
+                *(f32x4*)(to + 4 * h) = v;
+            }
+        }
+    }
+};
 
 // x as QL bf16 numbers whose sum it is: bf16 has one, fp16 8 + 3 bits, fp32 three times 8.
 template <int QL>

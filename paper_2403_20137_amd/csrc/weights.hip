@@ -26,6 +26,7 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
     __shared__ __align__(16) float q_s[16 * kQStride];
     __shared__ int perm_s[kD];
     __shared__ int depth_s[64];
+    __shared__ RowRule rule_s[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
     const int b = blockIdx.z, kvh = blockIdx.y;
@@ -56,10 +57,12 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < a.M; r0 += 16) {
+        QueryRows<QL, 16> rows;
+        rows.request(a, b, kvh, r0);
         __syncthreads();
-        stage_queries<QL, 16>(a, b, kvh, r0, q_s, perm_s);
+        rows.put(a, r0, q_s, perm_s);
         const int r = r0 + l16;
-        const RowRule u = row_rule(a, s, b, kvh, r);
+        if (wave == 0 && group == 0) rule_s[l16] = row_rule(a, s, b, kvh, r);
         float lse = -INFINITY;
         if (r < a.M) {
             const int tok = r / a.G;
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i];
         }
-        const float factor = rule_scores<8, true>(a, s, u, depth_s, false, t0 + 4 * group, mul, y);
+        const float factor = rule_scores<8, true>(a, s, rule_s + l16, depth_s, false, t0 + 4 * group, mul, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(fmaf(y[i], factor, -ref)) : 0.f;
     }
