@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkvbfp.so")
-SOURCES = ["host_ops.cpp", "quantize.hip", "attention.hip", "decode_mfma.hip", "decode_mfma_p8.hip", "decode_rope.hip", "decode_rope_f32.hip", "decode_wide.hip", "decode_scored.hip", "weights.hip",
+SOURCES = ["decode_scored.hip", "host_ops.cpp", "quantize.hip", "attention.hip", "decode_mfma.hip", "decode_mfma_p8.hip", "decode_rope.hip", "decode_rope_f32.hip", "decode_wide.hip", "weights.hip",
            "evict.hip", "measure.hip"]
 
 HIPCC_FLAGS = [

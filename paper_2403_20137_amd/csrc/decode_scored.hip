@@ -237,9 +237,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     const auto tiles = tiles_of<kTileTokens>(s, lo_least);
     const int last16 = (s.len - 1) & ~15;
     Chunk<P, N16> k_next[2], v_next[2];
+    // (without a branch: a load whose result meets another value behind it would be waited for there.  Tokens behind the last one and
+    // tiles behind the last one stand for something that is read anyway.)
     auto request = [&](int v) {
         const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
-        if (v >= tiles.count || t0 >= s.len) return;         // (uniform for the wavefront)
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const int from = min(t0 + 16 * st, last16);
@@ -249,7 +250,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_next[st]);
         }
     };
-    request(place.split);
+    const bool some = place.split < tiles.count;             // (else there may be no token at all)
+    if (some) request(place.split);
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
     rows.put(a, 0, (float*)smem, perm_s);
     if (tid < 16) rule_s[tid] = row_rule(a, s, b, kvh, tid);
@@ -271,7 +273,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         Chunk<P, N16> kc[2], vc[2];
 #pragma unroll
         for (int st = 0; st < 2; ++st) { kc[st] = k_next[st]; vc[st] = v_next[st]; }
-        request(v + n_splits);
+        request(v + n_splits < tiles.count ? v + n_splits : v);
         float y[1][8];
         products<QL, 1>([&](int st, int j) { return __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j)); }, q, y);
 #pragma unroll
@@ -325,15 +327,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int last16 = (s.len - 1) & ~15;
     // a thread decodes 32 channels of one token, keys and values: wavefront w tokens 16 w ..
     Chunk<P, N16> k_raw, v_raw;
-    auto request = [&](int v) {
-        if (v >= tiles.count) return;
+    auto request = [&](int v) {                              // (without a branch, as in scored_split)
         const int t0 = tiles.at(v) * kWideTokens + 16 * wave, from = min(t0, last16);
         const int off = min(t0 + l16, s.len - 1) - from;
         const int64_t row = stage_row(a, b, kvh, from);
         load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_raw);
         load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_raw);
     };
-    request(place.split);
+    if (place.split < tiles.count) request(place.split);
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
     if (tid < 2) large_s[tid] = 0;
     for (int i = tid; i < 16 * RW * HC; i += kThreads) rule_s[i] = row_rule(a, s, b, kvh, r0 + i);
@@ -364,15 +365,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(v_raw, j);
         if (__builtin_amdgcn_ballot_w64(has_large(v_raw)) && lane == 0) large_s[half] = 1;
     };
-    if (place.split < tiles.count) decode(0);
-    request(place.split + n_splits);
+    const auto after = [&](int v) { return v + n_splits < tiles.count ? v + n_splits : v; };
+    if (place.split < tiles.count) {
+        decode(0);
+        request(after(place.split));
+    }
     int half = 0;
     float slack = kSlack;
     for (int v = place.split; v < tiles.count; v += n_splits, half ^= 1) {
         __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
         if (v + n_splits < tiles.count) decode(half ^ 1);
-        request(v + 2 * n_splits);
+        request(after(after(v)));
         if (large_s[half]) slack = 0.f;
         // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
 #pragma unroll 1

@@ -262,6 +262,38 @@ __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const 
     return factor;
 }
 
+// The same for N rows (rule_s[0] ..) of one token t, exactly; everything multiplied.
+template <int N>
+__device__ __forceinline__ void rule_token(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t, float mul, float (&y)[N]) {
+    if (a.cap != 0.f) {
+        cap_scores<N, true>(y, mul, a.cap, a.inv_cap);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] *= mul;
+    }
+    if (inner) {
+        if (a.slopes) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] = fmaf(-rule_s[i].slope, (float)(rule_s[i].pos - t), y[i]);
+        }
+        return;
+    }
+    const int node = t - s.base;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const RowRule u = rule_s[i];
+        bool seen = t >= u.lo;
+        int far = u.pos - t;
+        if (node >= 0) {
+            far = u.pos - s.base - depth_s[node & 63];
+            seen = ((u.nodes >> (node & 63)) & 1) && t >= u.first && (a.window == 0 || far < a.window);
+        }
+        seen = (seen || t < s.prefix) && t < s.len;
+        if (a.slopes) y[i] = fmaf(-u.slope, fabsf((float)far), y[i]);
+        y[i] = seen ? y[i] : -INFINITY;
+    }
+}
+
 // 32 channels of one cached row, as loaded: lane (row l % 16 of a stage of 16 tokens, chunk l / 16).  N16: blocks of 16, two in a chunk.
 template <int P, bool N16>
 struct Chunk {

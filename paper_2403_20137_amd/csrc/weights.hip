@@ -1,8 +1,10 @@
 // The attention weights that cached tokens collect (kvbfp_accumulate_weights and its paged form):
 //     w_out[b][h][t] = decay * w_in[b][h][t] + sum over the rows of kv-head h of exp(score(row, t) - lse(row)),
 // scores and rule as in decode_scored.hip, whose lse it takes: a second pass over the keys alone, without any exchange between tokens.
-// A wavefront holds the keys of 32 tokens as matrix operands and goes through the rows 16 at a time; a lane sums the weights of its
-// row's column in registers, the 16 columns are added at the end: no atomics, the same bits every time.
+// S = Q K^T by v_mfma_f32_16x16x32_bf16: a lane has four rows of one token, so the sum over the rows stays in the lane, and the four 16-lane
+// groups are added once at the end: no atomics, the same bits every time.  A wavefront has 32 tokens at a time as operands (the keys go
+// from memory to the operand, 32 channels a lane) and goes through up to 128 rows (fp32 I/O 64), which lie in LDS as operands; more rows are further
+// passes over the keys, which add to what the pass before has written.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -17,93 +19,163 @@ namespace {
 using namespace kvbfp::scored;
 
 constexpr int kThreads = 256;
-constexpr int kWaveTokens = 32;
-constexpr int kTileTokens = 128;
+constexpr int kStages = 2;                       // of 16 tokens, per wavefront
+constexpr int kWaveTokens = 16 * kStages;
+constexpr int kTileTokens = 4 * kWaveTokens;
 
-// grid = (tiles of 128 tokens, H_kv, B)
+// grid = (n_splits * B, H_kv); QL bf16 numbers of a query
 template <int P, bool N16, int QL>
-__global__ __launch_bounds__(kThreads) void accumulate_weights(Args a) {
-    __shared__ __align__(16) float q_s[16 * kQStride];
-    __shared__ int perm_s[kD];
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void accumulate_weights(Args a) {
+    typedef typename Io<QL>::T T;
+    typedef T Tx8 __attribute__((ext_vector_type(8)));
+    constexpr int kChunk = QL == 3 ? 64 : 128;                   // rows in LDS
+    __shared__ __align__(16) uint8_t q_s[QL][kChunk * 256];      // rows in the order of eight(), 16-byte pieces exchanged by the row
+    __shared__ RowRule rule_s[kChunk];
+    __shared__ float ref_s[kChunk];                              // -lse in base 2; minus infinity: the row has no weights to give
+    __shared__ int at_s[kD];                                     // position of a channel of the query
     __shared__ int depth_s[64];
-    __shared__ RowRule rule_s[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
-    const int b = blockIdx.z, kvh = blockIdx.y;
+    const Place place = place_at(a, blockIdx.x);
+    if (place.split < 0) return;
+    const int b = place.b, kvh = blockIdx.y;
     const Seq s = sequence(a, b);
-    if ((int)blockIdx.x * kTileTokens >= s.len) return;                  // (uniform for the workgroup)
-    const int t0 = (int)blockIdx.x * kTileTokens + wave * kWaveTokens;
-    const bool some = t0 < s.len;
-    const int last16 = (s.len - 1) & ~15;
-
-    Chunk<P, N16> kc[2];
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {                                     // (a wavefront behind the last token reads the last stage)
-        const int from = min(t0 + 16 * st, last16);
-        const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
-        load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), off, group, kc[st]);
-    }
-    // token of this lane in the store, and what it has so far
-    const int t_mine = t0 + lane;
+    const int tiles = (s.len + kTileTokens - 1) / kTileTokens, last16 = (s.len - 1) & ~15;
+    if (place.split >= tiles) return;                            // (uniform for the workgroup)
     const int64_t unit = (int64_t)b * a.H_kv + kvh;
-    const bool mine = lane < kWaveTokens && t_mine < s.len;
-    const float before = mine && a.w_in ? a.w_in[unit * a.w_stride + t_mine] : 0.f;
-    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    bf16x8 k[2][4];
-#pragma unroll
-    for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k[st][j] = __builtin_bit_cast(bf16x8, eight<P, N16>(kc[st], j));
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < a.M; r0 += 16) {
-        QueryRows<QL, 16> rows;
-        rows.request(a, b, kvh, r0);
-        __syncthreads();
-        rows.put(a, r0, q_s, perm_s);
-        const int r = r0 + l16;
-        if (wave == 0 && group == 0) rule_s[l16] = row_rule(a, s, b, kvh, r);
-        float lse = -INFINITY;
-        if (r < a.M) {
-            const int tok = r / a.G;
-            lse = a.lse_in[((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)];
+
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    if (tid < kD) at_s[tid] = tid;                               // (what is no permutation leaves no entry out)
+    __syncthreads();
+    if (tid < kD) {
+        const int channel = position_channel<P>(tid);
+        at_s[a.perm_k ? a.perm_k[kvh * kD + channel] & (kD - 1) : channel] = tid;
+    }
+    for (int r0 = 0; r0 < a.M; r0 += kChunk) {
+        int lo_least, lo_most;
+        row_limits(a, s, b, r0, kChunk, lo_least, lo_most);
+        struct Tile {
+            Chunk<P, N16> raw[kStages];
+            float before;                                        // what the lane's token has so far
+        } next[2];                                               // two tiles in flight
+        auto sees = [&](int t0) { return t0 < s.len && (t0 < s.prefix || t0 + kWaveTokens > min(lo_least, max(s.base, 0))); };
+        // (without a branch: a load whose result meets another value behind it would be waited for there.  Tiles behind the last one and
+        // those that no row sees stand for something that is read anyway.)
+        auto request = [&](int v, Tile& to) {
+            v = min(v, tiles - 1);
+            int t0 = v * kTileTokens + wave * kWaveTokens;
+            const int64_t mine = unit * a.w_stride + min(t0 + min(lane, kWaveTokens - 1), s.len - 1);
+            to.before = *(r0 > 0 ? a.w_out + mine : a.w_in ? a.w_in + mine : a.lse_in);
+            t0 = sees(t0) ? t0 : last16;
+#pragma unroll
+            for (int st = 0; st < kStages; ++st) {
+                const int from = min(t0 + 16 * st, last16);
+                const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
+                load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), off, group, to.raw[st]);
+            }
+        };
+        request(place.split, next[0]);
+        request(place.split + place.n, next[1]);
+        __syncthreads();                                         // at_s is complete; nobody looks at the rows before these any more
+        const int rows = min(a.M - r0, kChunk), groups = (rows + 15) / 16;
+        const bool vec = ((uintptr_t)a.q & 15u) == 0;
+        for (int i = tid; i < groups * 256; i += kThreads) {
+            const int row = i >> 4, c = (i & 15) * 8, r = min(r0 + row, a.M - 1), tok = r / a.G;
+            const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
+            Tx8 x;
+            if (vec) {
+                x = *(const Tx8*)src;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = src[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                __bf16 l[QL];
+                limbs<QL>((float)x[k], l);
+                const int p = at_s[c + k];
+#pragma unroll
+                for (int n = 0; n < QL; ++n) *(__bf16*)(q_s[n] + row * 256 + (((p >> 3) ^ (row & 15)) * 16) + (p & 7) * 2) = l[n];
+            }
+        }
+        if (tid < kChunk) {
+            const int r = r0 + tid;
+            rule_s[tid] = row_rule(a, s, b, kvh, r);
+            float ref = -INFINITY;
+            if (r < a.M) {
+                const int tok = r / a.G;
+                const float lse = a.lse_in[((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)];
+                if (lse != -INFINITY) ref = -lse * 1.4426950408889634f;
+            }
+            ref_s[tid] = ref;
         }
         __syncthreads();
-        bf16x8 q[QL][4];
-        query_operand<P, QL>(q_s, perm_s, l16, group, q);
-        const bool counts = lse > -INFINITY;                             // a row that saw nothing has no weights to give
-        const float ref = counts ? lse * 1.4426950408889634f : 0.f;
-        float y[8];
+        auto step = [&](int v, Tile& from) {
+            const int t0 = v * kTileTokens + wave * kWaveTokens;
+            if (t0 >= s.len) return;
+            float* const w_out = a.w_out + unit * a.w_stride + t0 + lane;
+            const bool mine = lane < kWaveTokens && t0 + lane < s.len;
+            const float before = from.before;                    // (not multiplied before it is used: that would wait for it)
+            float acc[kStages] = {};
+            const bool seen = sees(t0), inner = t0 >= lo_most && t0 + kWaveTokens <= s.base;
+            bf16x8 k[kStages][4];
+            if (seen) {
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+                for (int st = 0; st < kStages; ++st)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 4; ++j) k[st][j] = __builtin_bit_cast(bf16x8, eight<P, N16>(from.raw[st], j));
+            }
+            request(v + 2 * place.n, from);
+            for (int g = 0; seen && g < groups; ++g) {
+                f32x4 sc[kStages];
 #pragma unroll
-                for (int i = 0; i < QL; ++i) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[st][j], q[i][j], sc, 0, 0, 0);
+                for (int st = 0; st < kStages; ++st) sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[4 * st + i] = sc[i];
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < QL; ++n) {
+                        const bf16x8 q = *(const bf16x8*)(q_s[n] + (16 * g + l16) * 256 + (((4 * group + j) ^ l16) * 16));
+#pragma unroll
+                        for (int st = 0; st < kStages; ++st) sc[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k[st][j], sc[st], 0, 0, 0);
+                    }
+                const f32x4 ref = *(const f32x4*)(ref_s + 16 * g + 4 * group);
+                if (a.cap == 0.f && !a.slopes && inner) {
+#pragma unroll
+                    for (int st = 0; st < kStages; ++st)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[st] += exp2_raw(fmaf(sc[st][i], mul, ref[i]));
+                } else {
+#pragma unroll
+                    for (int st = 0; st < kStages; ++st) {
+                        float y[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = sc[st][i];
+                        rule_token<4>(a, s, rule_s + 16 * g + 4 * group, depth_s, inner, t0 + 16 * st + l16, mul, y);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[st] += exp2_raw(y[i] + ref[i]);
+                    }
+                }
+            }
+            // lane: token 16 group + l16
+            float got = 0.f;
+#pragma unroll
+            for (int st = 0; st < kStages; ++st) {
+                const float sum = rows_sum(acc[st]);
+                if (group == st) got = sum;
+            }
+            if (mine) *w_out = r0 > 0 ? before + got : a.w_in ? fmaf(a.decay, before, got) : got;
+        };
+        for (int v = place.split; v < tiles; v += 2 * place.n) {
+            step(v, next[0]);
+            step(v + place.n, next[1]);
         }
-        const float factor = rule_scores<8, true>(a, s, rule_s + l16, depth_s, false, t0 + 4 * group, mul, y);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] += counts ? exp2_raw(fmaf(y[i], factor, -ref)) : 0.f;
     }
-    if (!some) return;
-    // acc[4 st + i] of the 16 lanes of a group: token t0 + 16 st + 4 group + i
-    float got = 0.f;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-        const float sum = row_sum(acc[x]);
-        // token 16 (x / 4) + 4 g + x % 4 is stored by the lane of that number
-        const float there = __shfl(sum, ((lane >> 2) & 3) * 16);
-        if (((lane >> 4) & 1) == (x >> 2) && (lane & 3) == (x & 3)) got = there;
-    }
-    if (mine) a.w_out[unit * a.w_stride + t_mine] = fmaf(a.decay, before, got);
 }
 
 template <int P, bool N16>
 void launch(const Args& a, int dt, hipStream_t s) {
-    const dim3 grid((unsigned)((a.max_len + kTileTokens - 1) / kTileTokens), (unsigned)a.H_kv, (unsigned)a.batch);
+    const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)a.H_kv);
     if (dt == KVBFP_F32) accumulate_weights<P, N16, 3><<<grid, kThreads, 0, s>>>(a);
     else if (dt == KVBFP_F16) accumulate_weights<P, N16, 2><<<grid, kThreads, 0, s>>>(a);
     else accumulate_weights<P, N16, 1><<<grid, kThreads, 0, s>>>(a);
@@ -129,6 +201,10 @@ static int weights_impl(const char* call, const kvbfp_layout* L, const kvbfp_cac
     if (a.H_kv > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     a.perm_k = perm_k;
     a.lse_in = lse; a.w_in = weights_in; a.w_out = weights_out; a.w_stride = weights_stride; a.decay = decay;
+    // three workgroups per compute unit
+    const int64_t tiles = (max_len + kTileTokens - 1) / kTileTokens, units = (int64_t)a.batch * a.H_kv;
+    a.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (768 + units - 1) / units));
+    a.share = seq_len_dev && a.batch > 1 && a.batch <= 64 && a.n_splits > 1;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool n16 = logical.block == 16;
     if (logical.mant_bits == 4) {
