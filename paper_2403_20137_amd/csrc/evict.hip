@@ -1,9 +1,11 @@
 // Eviction of cached tokens by the weight they have collected (kvbfp_evict and its paged form): per sequence and kv-head the first n_first
 // tokens, the last n_recent and those with the largest weights between them stay, n_keep in all, and go in their order to another cache.
 //
-// Selection (evict_select), a workgroup per sequence and kv-head: the weight of the last one that stays is found by its bits, eight at
-// a time from the top (a histogram of those that agree in the bits so far), ties go to the lowest index, and what stays is written
-// in order by prefix counts.  Rows (evict_rows): 16 bytes a thread.
+// Selection (evict_select), a workgroup of 16 wavefronts per sequence and kv-head, each with a stretch of the tokens, up to 2048 of
+// it in LDS: the weight of the last one that stays is found by its bits, eleven at a time from the top (a histogram in LDS of
+// those that agree in the bits so far; the search ends as soon as all that agree stay), ties go to the lowest index, and what stays is
+// written in order by counts of the wavefronts' ballots.  Bound by the passes' barriers and LDS atomics, not by the reading: SELECT_FIGURE.
+// Rows (evict_rows): 16 bytes a thread and plane, two rows in flight.  Bound by memory: ROWS_FIGURE.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,27 +33,56 @@ struct EvictArgs {
     int32_t* kept;                       // [B][H][n_keep]
     int32_t* new_len;                    // [B]
     float* w_out;                        // [B][H][n_keep] or nullptr
-    int32_t mant_bytes, n_exps;          // of a row
+    int32_t n_exps;                      // of a row
+    int32_t held;                        // keys of a lane that have room in LDS
 };
 
 __device__ __forceinline__ int length_of(const EvictArgs& a, int b) {
     return a.seq_len ? min(max(a.seq_len[b], 0), a.max_len) : a.max_len;
 }
 
-// Weights in the order of unsigned integers: NaN lowest, both zeros alike.
-__device__ __forceinline__ uint32_t key_of(float w) {
-    if (w != w) return 0u;
+// Weights in the order of unsigned integers: NaN lowest, both zeros alike; tokens that stay anyway above all others, and what lies behind
+// the last token like NaN (its index is larger than theirs, and there are enough others).
+__device__ __forceinline__ uint32_t key_of(float w, int t, int lo, int hi, int len) {
     const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t k = w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+    return t >= lo && t < hi ? k : t < len ? ~0u : 0u;
+}
+
+constexpr int kHeld = 32;                                  // keys of a lane in LDS
+constexpr int kBins = 2048;
+
+// f(i, key) for the tokens from + 64 i + lane of a wavefront's stretch, i < n, in order: the first keys are in LDS (held: this
+// wavefront's, 64 times kHeld at most), others are read again, eight in flight.  `from` + 64 n may lie beyond `len`.
+template <class F>
+__device__ __forceinline__ void each_key(const uint32_t* held, int n, const float* w, int from, int lo, int hi, int len, F&& f) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 8) {
+        uint32_t k[8];
+        if (i0 < kHeld) {                                  // (kHeld is a multiple of 8; what was not put there is not looked at)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k[i] = held[64 * min(i0 + i, n - 1) + lane];
+        } else {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = w[min(from + 64 * (i0 + i) + lane, len - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k[i] = key_of(x[i], from + 64 * (i0 + i) + lane, lo, hi, len);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i0 + i < n) f(i0 + i, k[i]);
+    }
 }
 
 // grid = (H, B)
 __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
-    __shared__ int hist_s[256];
+    extern __shared__ uint32_t held_s[];                   // [wavefronts][a.held][64]
+    __shared__ int hist_s[kBins];
     __shared__ int wave_s[kWaves][2];
-    __shared__ uint32_t prefix_s;
-    __shared__ int left_s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int found_s[3];                             // digit, how many are above it, how many it has
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = blockIdx.x, b = blockIdx.y;
     const int len = length_of(a, b), unit = b * a.H + h;
     const int count = min(len, a.n_keep);
@@ -63,68 +94,65 @@ __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
         return;
     }
     const float* const w = a.weights + (int64_t)unit * a.w_stride;
-    const int lo = a.n_first, hi = len - a.n_recent;       // candidates [lo, hi); more than are needed
-    int need = a.n_keep - a.n_first - a.n_recent;
+    const int lo = a.n_first, hi = len - a.n_recent;       // the others stay anyway
+    int need = a.n_keep;                                   // of those that agree with `bits` where it is known
     uint32_t bits = 0, known = 0;                          // of the smallest key that stays
-    if (need > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kThreads) hist_s[i] = 0;
-            __syncthreads();
-            for (int t = lo + tid; t < hi; t += kThreads) {
-                const uint32_t k = key_of(w[t]);
-                if ((k & known) == bits) atomicAdd(&hist_s[(k >> shift) & 255u], 1);
-            }
-            __syncthreads();
-            if (wave == 0) {                               // the digit in which the need-th largest lies: sums from the top
-                int mine[4], total = 0;
-                for (int i = 0; i < 4; ++i) {
-                    mine[i] = hist_s[255 - (4 * lane + i)];
-                    total += mine[i];
-                }
-                int before = total;                        // inclusive sum over the lanes, then exclusive
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int up = __shfl_up(before, d);
-                    if (lane >= d) before += up;
-                }
-                before -= total;
-                for (int i = 0; i < 4; ++i) {
-                    if (before < need && need <= before + mine[i]) {
-                        prefix_s = bits | ((uint32_t)(255 - (4 * lane + i)) << shift);
-                        left_s = need - before;
-                    }
-                    before += mine[i];
-                }
-            }
-            __syncthreads();
-            bits = prefix_s;
-            need = left_s;                                 // of those that agree with `bits`
-            known |= 255u << shift;
-            __syncthreads();
-        }
-    }
-    // in order: every wavefront a stretch of the tokens; what it keeps and how many ties it has, then where they go
     const int stretch = ((len + kWaves - 1) / kWaves + 63) & ~63;
-    const int from = min(wave * stretch, len), to = min(from + stretch, len);
-    const bool by_weight = a.n_keep - a.n_first - a.n_recent > 0;
-    auto look = [&](int t, bool& more, bool& tie) {
-        more = tie = false;
-        if (t >= to) return;
-        if (t < lo || t >= hi) {
-            more = true;
-            return;
-        }
-        if (!by_weight) return;
-        const uint32_t k = key_of(w[t]);
-        more = k > bits;
-        tie = k == bits;
-    };
-    int n_more = 0, n_tie = 0;
-    for (int t = from; t < to; t += 64) {
-        bool more, tie;
-        look(t + lane, more, tie);
-        n_more += __popcll(__ballot(more));
-        n_tie += __popcll(__ballot(tie));
+    const int from = min(wave * stretch, len), to = min(from + stretch, len), n = (to - from + 63) / 64;
+    uint32_t* const held = held_s + wave * (64 * a.held);
+#pragma unroll 1
+    for (int i0 = 0; i0 < min(n, kHeld); i0 += 16) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = w[min(from + 64 * (i0 + i) + lane, len - 1)];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i0 + i < min(n, kHeld)) held[64 * (i0 + i) + lane] = key_of(x[i], from + 64 * (i0 + i) + lane, lo, hi, len);
     }
+    for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {         // 11, 11 and 10 bits
+        const uint32_t digits = shift == 0 ? 1023u : 2047u;
+        for (int i = tid; i < kBins; i += kThreads) hist_s[i] = 0;
+        __syncthreads();
+        each_key(held, n, w, from, lo, hi, len, [&](int, uint32_t k) {
+            if ((k & known) == bits) atomicAdd(&hist_s[(k >> shift) & digits], 1);
+        });
+        __syncthreads();
+        // the digit in which the need-th largest lies: thread i has the bins 2047 - 2 i and 2046 - 2 i, sums from the top
+        const int2 mine = *(const int2*)(hist_s + kBins - 2 - 2 * tid);
+        const int total = mine.x + mine.y;
+        int before = total;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(before, d);
+            if (lane >= d) before += up;
+        }
+        if (lane == 63) wave_s[wave][0] = before;
+        __syncthreads();
+        before -= total;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) before += i < wave ? wave_s[i][0] : 0;
+        if (before < need && need <= before + mine.y) {
+            found_s[0] = kBins - 1 - 2 * tid;
+            found_s[1] = before;
+            found_s[2] = mine.y;
+        } else if (before + mine.y < need && need <= before + total) {
+            found_s[0] = kBins - 2 - 2 * tid;
+            found_s[1] = before + mine.y;
+            found_s[2] = mine.x;
+        }
+        __syncthreads();
+        bits |= (uint32_t)found_s[0] << shift;
+        known |= digits << shift;
+        need -= found_s[1];
+        if (need == found_s[2] || shift == 0) break;   // all that agree stay, or there is nothing left to tell them apart
+    }
+    // in order: what every wavefront keeps and how many ties it has, then where they go
+    int n_more = 0, n_tie = 0;
+    each_key(held, n, w, from, lo, hi, len, [&](int, uint32_t k) {
+        n_more += __popcll(__ballot((k & known) > bits));
+        n_tie += __popcll(__ballot((k & known) == bits));
+    });
+    __syncthreads();                                       // (nobody looks at the sums of the last digit any more)
     if (lane == 0) {
         wave_s[wave][0] = n_more;
         wave_s[wave][1] = n_tie;
@@ -137,17 +165,16 @@ __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
     }
     at += min(ties, need);
     const uint64_t below = (1ull << lane) - 1;
-    for (int t = from; t < to; t += 64) {
-        bool more, tie;
-        look(t + lane, more, tie);
+    each_key(held, n, w, from, lo, hi, len, [&](int i, uint32_t k) {
+        const bool tie = (k & known) == bits;
         const uint64_t all_ties = __ballot(tie);
-        const bool stays = more || (tie && ties + __popcll(all_ties & below) < need);
+        const bool stays = (k & known) > bits || (tie && ties + __popcll(all_ties & below) < need);
         const uint64_t all = __ballot(stays);
         const int place = at + __popcll(all & below);
-        if (stays && place < a.n_keep) kept[place] = t + lane;
+        if (stays && place < a.n_keep) kept[place] = from + 64 * i + lane;
         at += __popcll(all);
         ties += __popcll(all_ties);
-    }
+    });
 }
 
 __device__ __forceinline__ int64_t row_of(const int32_t* table, int64_t stride, int log2_page, int pages, int64_t seq, int H, int b, int h, int t) {
@@ -156,26 +183,53 @@ __device__ __forceinline__ int64_t row_of(const int32_t* table, int64_t stride, 
     return (((int64_t)page * H + h) << log2_page) + (t & ((1 << log2_page) - 1));
 }
 
-// A group of PER threads per kept row: 16 bytes of the key and of the value row each, and the exponents.  grid = (rows / (256 / PER), H, B)
+// PER threads have 16 bytes each of the key and of the value row of two kept tokens.  grid = (rows / (512 / PER), H, B)
 template <int PER>
 __global__ __launch_bounds__(256) void evict_rows(EvictArgs a) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const int i = (blockIdx.x * 256 + threadIdx.x) / PER, part = threadIdx.x % PER;
+    constexpr int kRows = 2, kGroup = 256 / PER;
+    const int part = threadIdx.x % PER, i0 = blockIdx.x * (kRows * kGroup) + threadIdx.x / PER;
     const int h = blockIdx.y, b = blockIdx.z;
-    if (i >= min(length_of(a, b), a.n_keep)) return;       // (what lies behind the last kept token stays as it was)
+    const int count = min(length_of(a, b), a.n_keep);
     const int64_t unit = (int64_t)b * a.H + h;
-    const int t = min(max(a.kept[unit * a.n_keep + i], 0), a.max_len - 1);
-    const int64_t from = row_of(a.src_table, a.src_stride, a.src_log2_page, a.src_pages, a.src_seq, a.H, b, h, t);
-    const int64_t to = row_of(a.dst_table, a.dst_stride, a.dst_log2_page, a.dst_pages, a.dst_seq, a.H, b, h, i);
-    const u32x4 k = *(const u32x4*)(a.src[0] + from * (PER * 16) + part * 16);
-    const u32x4 v = *(const u32x4*)(a.src[2] + from * (PER * 16) + part * 16);
-    *(u32x4*)(a.dst[0] + to * (PER * 16) + part * 16) = k;
-    *(u32x4*)(a.dst[2] + to * (PER * 16) + part * 16) = v;
-    for (int e = part; e < a.n_exps; e += PER) {
-        a.dst[1][to * a.n_exps + e] = a.src[1][from * a.n_exps + e];
-        a.dst[3][to * a.n_exps + e] = a.src[3][from * a.n_exps + e];
+    int t[kRows];
+    int64_t from[kRows], to[kRows];
+    u32x4 k[kRows], v[kRows];
+    uint8_t ke[kRows], ve[kRows];
+    float w[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) t[r] = a.kept[unit * a.n_keep + min(i0 + r * kGroup, max(count - 1, 0))];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int i = i0 + r * kGroup;
+        if (i >= count) continue;                          // (what lies behind the last kept token stays as it was)
+        t[r] = min(max(t[r], 0), a.max_len - 1);
+        from[r] = row_of(a.src_table, a.src_stride, a.src_log2_page, a.src_pages, a.src_seq, a.H, b, h, t[r]);
+        to[r] = row_of(a.dst_table, a.dst_stride, a.dst_log2_page, a.dst_pages, a.dst_seq, a.H, b, h, i);
+        k[r] = *(const u32x4*)(a.src[0] + from[r] * (PER * 16) + part * 16);
+        v[r] = *(const u32x4*)(a.src[2] + from[r] * (PER * 16) + part * 16);
+        if (part < a.n_exps) {                             // (n_exps <= 8; with PER = 4 the other half below)
+            ke[r] = a.src[1][from[r] * a.n_exps + part];
+            ve[r] = a.src[3][from[r] * a.n_exps + part];
+        }
+        if (a.w_out && part == 0) w[r] = a.weights[unit * a.w_stride + t[r]];
     }
-    if (a.w_out && part == 0) a.w_out[unit * a.n_keep + i] = a.weights[unit * a.w_stride + t];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int i = i0 + r * kGroup;
+        if (i >= count) continue;
+        *(u32x4*)(a.dst[0] + to[r] * (PER * 16) + part * 16) = k[r];
+        *(u32x4*)(a.dst[2] + to[r] * (PER * 16) + part * 16) = v[r];
+        if (part < a.n_exps) {
+            a.dst[1][to[r] * a.n_exps + part] = ke[r];
+            a.dst[3][to[r] * a.n_exps + part] = ve[r];
+        }
+        if (PER < 8 && part + PER < a.n_exps) {            // blocks of 16, 4-bit mantissas
+            a.dst[1][to[r] * a.n_exps + part + PER] = a.src[1][from[r] * a.n_exps + part + PER];
+            a.dst[3][to[r] * a.n_exps + part + PER] = a.src[3][from[r] * a.n_exps + part + PER];
+        }
+        if (a.w_out && part == 0) a.w_out[unit * a.n_keep + i] = w[r];
+    }
 }
 
 }  // namespace
@@ -252,10 +306,11 @@ static int evict_impl(const char* call, const kvbfp_layout* L, const kvbfp_cache
     a.kept = kept; a.new_len = new_len; a.w_out = weights_out;
     a.n_exps = kD / from.block;
     hipStream_t s = (hipStream_t)hip_stream;
-    evict_select<<<dim3((unsigned)a.H, (unsigned)a.batch), kThreads, 0, s>>>(a);
+    a.held = (int32_t)std::min<int64_t>(kHeld, (max_len + kThreads - 1) / kThreads);
+    evict_select<<<dim3((unsigned)a.H, (unsigned)a.batch), kThreads, (size_t)a.held * kThreads * sizeof(uint32_t), s>>>(a);
     hipError_t err = hipGetLastError();
     if (err == hipSuccess) {
-        const int per = from.mant_bits, rows = 256 / per;                      // 64 or 128 bytes a row
+        const int per = from.mant_bits, rows = 512 / per;                      // 64 or 128 bytes a row
         const int64_t most = std::min<int64_t>(n_keep, max_len);
         const dim3 grid((unsigned)((most + rows - 1) / rows), (unsigned)a.H, (unsigned)a.batch);
         if (per == 4) evict_rows<4><<<grid, 256, 0, s>>>(a);
