@@ -5,7 +5,7 @@
 // it in LDS: the weight of the last one that stays is found by its bits, eleven at a time from the top (a histogram in LDS of
 // those that agree in the bits so far; the search ends as soon as all that agree stay), ties go to the lowest index, and what stays is
 // written in order by counts of the wavefronts' ballots.  Bound by the passes' barriers and LDS atomics, not by the reading: SELECT_FIGURE.
-// Rows (evict_rows): 16 bytes a thread and plane, two rows in flight.  Bound by memory: ROWS_FIGURE.
+// Rows (evict_rows): 16 bytes a thread and plane, four rows in flight.  Bound by memory: ROWS_FIGURE.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -44,42 +44,55 @@ __device__ __forceinline__ int length_of(const EvictArgs& a, int b) {
 // Weights in the order of unsigned integers: NaN lowest, both zeros alike; tokens that stay anyway above all others, and what lies behind
 // the last token like NaN (its index is larger than theirs, and there are enough others).
 __device__ __forceinline__ uint32_t key_of(float w, int t, int lo, int hi, int len) {
-    const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
-    const uint32_t k = w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
-    return t >= lo && t < hi ? k : t < len ? ~0u : 0u;
+    const uint32_t u = __float_as_uint(w + 0.f);
+    const uint32_t k = w != w ? 0u : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return (uint32_t)(t - lo) < (uint32_t)(hi - lo) ? k : t < len ? ~0u : 0u;
+}
+// COUNT weights 64 apart, from w[t] on; those behind the last token are the last one's.
+template <int COUNT>
+__device__ __forceinline__ void load_weights(const float* w, int t0, int lane, int len, float (&x)[COUNT]) {
+    if (t0 + 64 * COUNT <= len) {                          // (uniform: the addresses then differ by constants)
+        const float* const at = w + t0 + lane;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) x[i] = at[64 * i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) x[i] = w[min(t0 + 64 * i + lane, len - 1)];
+    }
+}
+__device__ __forceinline__ int bits_below(uint64_t m, int base) {          // base + bits of m below this lane's
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, (uint32_t)base));
 }
 
 constexpr int kHeld = 32;                                  // keys of a lane in LDS
 constexpr int kBins = 2048;
 
-// f(i, key) for the tokens from + 64 i + lane of a wavefront's stretch, i < n, in order: the first keys are in LDS (held: this
-// wavefront's, 64 times kHeld at most), others are read again, eight in flight.  `from` + 64 n may lie beyond `len`.
+// f(i, key) for the tokens from + 64 i + lane of a wavefront's stretch, i < n (a multiple of 8), in order: the first keys are in LDS (held:
+// this wavefront's, 64 times kHeld at most), others are read again, eight in flight.
 template <class F>
 __device__ __forceinline__ void each_key(const uint32_t* held, int n, const float* w, int from, int lo, int hi, int len, F&& f) {
     const int lane = threadIdx.x & 63;
 #pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += 8) {
         uint32_t k[8];
-        if (i0 < kHeld) {                                  // (kHeld is a multiple of 8; what was not put there is not looked at)
+        if (i0 < kHeld) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) k[i] = held[64 * min(i0 + i, n - 1) + lane];
+            for (int i = 0; i < 8; ++i) k[i] = held[64 * (i0 + i) + lane];
         } else {
             float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = w[min(from + 64 * (i0 + i) + lane, len - 1)];
+            load_weights<8>(w, from + 64 * i0, lane, len, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) k[i] = key_of(x[i], from + 64 * (i0 + i) + lane, lo, hi, len);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i0 + i < n) f(i0 + i, k[i]);
+        for (int i = 0; i < 8; ++i) f(i0 + i, k[i]);
     }
 }
 
 // grid = (H, B)
 __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
     extern __shared__ uint32_t held_s[];                   // [wavefronts][a.held][64]
-    __shared__ int hist_s[kBins];
+    __shared__ int hist_s[2 * kBins];                      // even and odd lanes: fewer of them meet in one bin
     __shared__ int wave_s[kWaves][2];
     __shared__ int found_s[3];                             // digit, how many are above it, how many it has
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -97,28 +110,40 @@ __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
     const int lo = a.n_first, hi = len - a.n_recent;       // the others stay anyway
     int need = a.n_keep;                                   // of those that agree with `bits` where it is known
     uint32_t bits = 0, known = 0;                          // of the smallest key that stays
-    const int stretch = ((len + kWaves - 1) / kWaves + 63) & ~63;
-    const int from = min(wave * stretch, len), to = min(from + stretch, len), n = (to - from + 63) / 64;
+    const int stretch = ((len + kWaves - 1) / kWaves + 511) & ~511;        // (whole groups of eight keys a lane)
+    const int from = min(wave * stretch, len), to = min(from + stretch, len), n = ((to - from + 511) & ~511) / 64;
     uint32_t* const held = held_s + wave * (64 * a.held);
-#pragma unroll 1
-    for (int i0 = 0; i0 < min(n, kHeld); i0 += 16) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = w[min(from + 64 * (i0 + i) + lane, len - 1)];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i0 + i < min(n, kHeld)) held[64 * (i0 + i) + lane] = key_of(x[i], from + 64 * (i0 + i) + lane, lo, hi, len);
-    }
+    int* const hist = hist_s + (lane & 1) * kBins;
     for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {         // 11, 11 and 10 bits
         const uint32_t digits = shift == 0 ? 1023u : 2047u;
-        for (int i = tid; i < kBins; i += kThreads) hist_s[i] = 0;
+        for (int i = tid; i < 2 * kBins; i += kThreads) hist_s[i] = 0;
         __syncthreads();
-        each_key(held, n, w, from, lo, hi, len, [&](int, uint32_t k) {
-            if ((k & known) == bits) atomicAdd(&hist_s[(k >> shift) & digits], 1);
-        });
+        if (shift == 21) {                                 // the first time: from memory, and all agree
+            float x[8], next[8];
+            load_weights<8>(w, from, lane, len, x);
+#pragma unroll 1
+            for (int i0 = 0; i0 < n; i0 += 8) {
+                load_weights<8>(w, from + 64 * min(i0 + 8, n - 8), lane, len, next);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t k = key_of(x[i], from + 64 * (i0 + i) + lane, lo, hi, len);
+                    if (i0 < kHeld) held[64 * (i0 + i) + lane] = k;
+                    atomicAdd(&hist[k >> 21], 1);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = next[i];
+            }
+        } else {
+            each_key(held, n, w, from, lo, hi, len, [&](int, uint32_t k) {
+                if ((k & known) == bits) atomicAdd(&hist[(k >> shift) & digits], 1);
+            });
+        }
         __syncthreads();
         // the digit in which the need-th largest lies: thread i has the bins 2047 - 2 i and 2046 - 2 i, sums from the top
-        const int2 mine = *(const int2*)(hist_s + kBins - 2 - 2 * tid);
+        int2 mine = *(const int2*)(hist_s + kBins - 2 - 2 * tid);
+        const int2 odd = *(const int2*)(hist_s + 2 * kBins - 2 - 2 * tid);
+        mine.x += odd.x;
+        mine.y += odd.y;
         const int total = mine.x + mine.y;
         int before = total;
 #pragma unroll
@@ -164,16 +189,17 @@ __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
         ties += wave_s[i][1];
     }
     at += min(ties, need);
-    const uint64_t below = (1ull << lane) - 1;
     each_key(held, n, w, from, lo, hi, len, [&](int i, uint32_t k) {
-        const bool tie = (k & known) == bits;
-        const uint64_t all_ties = __ballot(tie);
-        const bool stays = (k & known) > bits || (tie && ties + __popcll(all_ties & below) < need);
+        bool stays = (k & known) > bits;
+        const uint64_t all_ties = __ballot((k & known) == bits);
+        if (all_ties) {                                    // (uniform, and rare)
+            stays = stays || (((all_ties >> lane) & 1) && bits_below(all_ties, ties) < need);
+            ties += __popcll(all_ties);
+        }
         const uint64_t all = __ballot(stays);
-        const int place = at + __popcll(all & below);
+        const int place = bits_below(all, at);
         if (stays && place < a.n_keep) kept[place] = from + 64 * i + lane;
         at += __popcll(all);
-        ties += __popcll(all_ties);
     });
 }
 
@@ -183,11 +209,11 @@ __device__ __forceinline__ int64_t row_of(const int32_t* table, int64_t stride, 
     return (((int64_t)page * H + h) << log2_page) + (t & ((1 << log2_page) - 1));
 }
 
-// PER threads have 16 bytes each of the key and of the value row of two kept tokens.  grid = (rows / (512 / PER), H, B)
+// PER threads have 16 bytes each of the key and of the value row of four kept tokens.  grid = (rows / (1024 / PER), H, B)
 template <int PER>
 __global__ __launch_bounds__(256) void evict_rows(EvictArgs a) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    constexpr int kRows = 2, kGroup = 256 / PER;
+    constexpr int kRows = 4, kGroup = 256 / PER;
     const int part = threadIdx.x % PER, i0 = blockIdx.x * (kRows * kGroup) + threadIdx.x / PER;
     const int h = blockIdx.y, b = blockIdx.z;
     const int count = min(length_of(a, b), a.n_keep);
@@ -218,8 +244,8 @@ __global__ __launch_bounds__(256) void evict_rows(EvictArgs a) {
     for (int r = 0; r < kRows; ++r) {
         const int i = i0 + r * kGroup;
         if (i >= count) continue;
-        *(u32x4*)(a.dst[0] + to[r] * (PER * 16) + part * 16) = k[r];
-        *(u32x4*)(a.dst[2] + to[r] * (PER * 16) + part * 16) = v[r];
+        __builtin_nontemporal_store(k[r], (u32x4*)(a.dst[0] + to[r] * (PER * 16) + part * 16));
+        __builtin_nontemporal_store(v[r], (u32x4*)(a.dst[2] + to[r] * (PER * 16) + part * 16));
         if (part < a.n_exps) {
             a.dst[1][to[r] * a.n_exps + part] = ke[r];
             a.dst[3][to[r] * a.n_exps + part] = ve[r];
@@ -306,11 +332,11 @@ static int evict_impl(const char* call, const kvbfp_layout* L, const kvbfp_cache
     a.kept = kept; a.new_len = new_len; a.w_out = weights_out;
     a.n_exps = kD / from.block;
     hipStream_t s = (hipStream_t)hip_stream;
-    a.held = (int32_t)std::min<int64_t>(kHeld, (max_len + kThreads - 1) / kThreads);
+    a.held = (int32_t)std::min<int64_t>(kHeld, ((max_len + kThreads - 1) / kThreads + 7) / 8 * 8);
     evict_select<<<dim3((unsigned)a.H, (unsigned)a.batch), kThreads, (size_t)a.held * kThreads * sizeof(uint32_t), s>>>(a);
     hipError_t err = hipGetLastError();
     if (err == hipSuccess) {
-        const int per = from.mant_bits, rows = 512 / per;                      // 64 or 128 bytes a row
+        const int per = from.mant_bits, rows = 1024 / per;                     // 64 or 128 bytes a row
         const int64_t most = std::min<int64_t>(n_keep, max_len);
         const dim3 grid((unsigned)((most + rows - 1) / rows), (unsigned)a.H, (unsigned)a.batch);
         if (per == 4) evict_rows<4><<<grid, 256, 0, s>>>(a);
