@@ -45,9 +45,12 @@ __device__ __forceinline__ Tiles<TT> tiles_of(const Seq& s, int lo) {
     return t;
 }
 
-// Value rows in LDS: 256 bytes a token, the eight 32-byte segments of a row exchanged by its number so that 16 rows of
-// one segment lie in different banks.
-__device__ __forceinline__ int value_at(int row, int seg) { return row * 256 + ((seg ^ (row & 7)) * 32); }
+// Byte of a value row's 16-byte piece in LDS: 256 bytes a token; the eight 32-byte segments of a row are exchanged by its number, so that
+// 8 rows of one segment lie in different banks, and the halves of a segment by the number's next bit, so that 16 rows written at once
+// use all banks.
+__device__ __forceinline__ int value_at(int row, int seg, int half) {
+    return row * 256 + ((seg ^ (row & 7)) * 32) + ((half ^ ((row >> 3) & 1)) * 16);
+}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -58,11 +61,11 @@ __device__ __forceinline__ s16x4 read_by_channel(const uint8_t* p) {
 // o += V^T P^T for 32 tokens and HC times 16 rows: lane (row l % 16): probabilities of tokens 4 (l / 16) .. of either stage.
 template <int PL, int HC>
 __device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const bf16x8 (&p)[HC][PL], f32x4 (&o)[HC][8]) {
-    const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2), piece = (i & 3) * 8;
+    const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2), half = (i >> 1) & 1, word = (i & 1) * 8;
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) {
-        const s16x4 lo = read_by_channel(v_s + value_at(row, ct) + piece);
-        const s16x4 hi = read_by_channel(v_s + value_at(row + 16, ct) + piece);
+        const s16x4 lo = read_by_channel(v_s + value_at(row, ct, half) + word);
+        const s16x4 hi = read_by_channel(v_s + value_at(row + 16, ct, half) + word);
         const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
         for (int c = 0; c < HC; ++c)
@@ -239,15 +242,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     Chunk<P, N16> k_next[2], v_next[2];
     // (without a branch: a load whose result meets another value behind it would be waited for there.  Tokens behind the last one and
     // tiles behind the last one stand for something that is read anyway.)
+    const ChunkAt whole = chunk_at<P, N16>(a, l16, group);
     auto request = [&](int v) {
         const int t0 = tiles.at(v) * kTileTokens + wave * kWaveTokens;
+        ChunkAt at[2] = {whole, whole};
+        if (t0 + kWaveTokens > s.len) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st) at[st] = chunk_at<P, N16>(a, min(t0 + 16 * st + l16, s.len - 1) - min(t0 + 16 * st, last16), group);
+        }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            const int from = min(t0 + 16 * st, last16);
-            const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
-            const int64_t row = stage_row(a, b, kvh, from);
-            load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_next[st]);
-            load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_next[st]);
+            const int64_t row = stage_row(a, b, kvh, min(t0 + 16 * st, last16));
+            load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, at[st], k_next[st]);
+            load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, at[st], v_next[st]);
         }
     };
     const bool some = place.split < tiles.count;             // (else there may be no token at all)
@@ -280,7 +287,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(vc[st], j);
+                *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1), j & 1)) = eight<P, N16>(vc[st], j);
         if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) slack = 0.f;
         wave_fence();
         const float factor = rule_scores<8, QL == 3>(a, s, rule_s + l16, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, mul, y[0]);
@@ -326,13 +333,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const auto tiles = tiles_of<kWideTokens>(s, lo_least);
     const int last16 = (s.len - 1) & ~15;
     // a thread decodes 32 channels of one token, keys and values: wavefront w tokens 16 w ..
+    const ChunkAt whole = chunk_at<P, N16>(a, l16, group);
     Chunk<P, N16> k_raw, v_raw;
     auto request = [&](int v) {                              // (without a branch, as in scored_split)
         const int t0 = tiles.at(v) * kWideTokens + 16 * wave, from = min(t0, last16);
-        const int off = min(t0 + l16, s.len - 1) - from;
+        ChunkAt at = whole;
+        if (t0 + 16 > s.len) at = chunk_at<P, N16>(a, min(t0 + l16, s.len - 1) - from, group);
         const int64_t row = stage_row(a, b, kvh, from);
-        load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, off, group, k_raw);
-        load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, off, group, v_raw);
+        load_chunk<P, N16>(a, a.k_mant, a.k_exp, row, at, k_raw);
+        load_chunk<P, N16>(a, a.v_mant, a.v_exp, row, at, v_raw);
     };
     if (place.split < tiles.count) request(place.split);
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
@@ -362,7 +371,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + key_at(row, 4 * group + j)) = eight<P, N16>(k_raw, j);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1)) + (j & 1) * 16) = eight<P, N16>(v_raw, j);
+        for (int j = 0; j < 4; ++j) *(u32x4*)(tile + kPlane + value_at(row, 2 * group + (j >> 1), j & 1)) = eight<P, N16>(v_raw, j);
         if (__builtin_amdgcn_ballot_w64(has_large(v_raw)) && lane == 0) large_s[half] = 1;
     };
     const auto after = [&](int v) { return v + n_splits < tiles.count ? v + n_splits : v; };

@@ -68,6 +68,29 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
 // (n_splits each), or shared out by what the sequences have to read (up to 64 of them, a lane each): one each, the others in
 // proportion, rounded down, what is left by the largest remainders.
 struct Place { int b, split, n, first; };
+// Inclusive sum over the lanes of a wavefront: within the rows of 16 by shifts, then the rows' last sums into the rows behind them.  (Six
+// exchanges through LDS take six times its latency; 0 for a lane that nothing comes to.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    v += dpp_or_zero<0x143, 0xC>(v);
+    return v;
+}
+__device__ __forceinline__ float wave_scan(float v) {
+    auto step = [](int x) { return __int_as_float(x); };
+    v += step(dpp_or_zero<0x111, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x112, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x114, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x118, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x142, 0xA>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x143, 0xC>(__float_as_int(v)));
+    return v;
+}
 __device__ __forceinline__ int tokens_read(const Args& a, int b) {        // about: documents are not looked at
     int len = min(max(a.seq_len[b], 0), a.max_len);
     if (a.window) {
@@ -78,16 +101,12 @@ __device__ __forceinline__ int tokens_read(const Args& a, int b) {        // abo
 }
 __device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first) {
     const float mine = lane < a.batch ? (float)(tokens_read(a, lane) + 1) : 0.f;
-    float all = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+    const float all = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wave_scan(mine)), 63));
     const float extra = (float)((a.n_splits - 1) * a.batch);
     const float share = extra * (mine / all) * (1.f + 0x1p-20f);         // (a whole number stays one)
     n = lane < a.batch ? 1 + (int)share : 0;
-    int left = n;                        // the sum of rounded-down shares is at most what there is to share
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) left += __shfl_xor(left, d);
-    left = a.n_splits * a.batch - left;
+    // the sum of rounded-down shares is at most what there is to share
+    const int left = a.n_splits * a.batch - __builtin_amdgcn_readlane(wave_scan(n), 63);
     const float rest = share - floorf(share);
     int before = 0;
     for (int j = 0; j < a.batch; ++j) {
@@ -95,13 +114,7 @@ __device__ __forceinline__ void share_places(const Args& a, int lane, int& n, in
         before += other > rest || (other == rest && j < lane);
     }
     if (lane < a.batch && before < left) ++n;
-    first = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int below = __shfl_up(first, d);
-        if (lane >= d) first += below;
-    }
-    first -= n;
+    first = wave_scan(n) - n;
 }
 // The place `at`; split = -1: nobody's.
 __device__ __forceinline__ Place place_at(const Args& a, int at) {
@@ -300,18 +313,20 @@ struct Chunk {
     u32x4 m[P / 4];
     uint32_t e[N16 ? 2 : 1];
 };
+// Where in a stage's rows a lane's chunk lies: bytes of the mantissa and of the exponent plane.  The same for every stage but the last.
+struct ChunkAt { uint32_t m, e; };
 template <int P, bool N16>
-__device__ __forceinline__ void load_chunk(const Args& a, const uint8_t* mant, const uint8_t* exps, int64_t row0, int off, int chunk, Chunk<P, N16>& c) {
-    const u32x4* m = (const u32x4*)(mant + row0 * (16 * P) + (uint32_t)(off * (16 * P) + chunk * (4 * P)));
+__device__ __forceinline__ ChunkAt chunk_at(const Args& a, int row, int chunk) {
+    return ChunkAt{(uint32_t)(row * (16 * P) + chunk * (4 * P)), (uint32_t)(row * a.n_exps + (N16 ? 2 * chunk : (chunk * 32) >> a.log2_block))};
+}
+template <int P, bool N16>
+__device__ __forceinline__ void load_chunk(const Args& a, const uint8_t* mant, const uint8_t* exps, int64_t row0, ChunkAt at, Chunk<P, N16>& c) {
+    const uint8_t* const m = mant + row0 * (16 * P);
+    const uint8_t* const e = exps + row0 * a.n_exps;
 #pragma unroll
-    for (int i = 0; i < P / 4; ++i) c.m[i] = __builtin_nontemporal_load(m + i);
-    const uint8_t* e = exps + row0 * a.n_exps + (uint32_t)(off * a.n_exps);
-    if (N16) {
-        c.e[0] = e[2 * chunk];
-        c.e[N16 ? 1 : 0] = e[2 * chunk + 1];
-    } else {
-        c.e[0] = e[(chunk * 32) >> a.log2_block];
-    }
+    for (int i = 0; i < P / 4; ++i) c.m[i] = __builtin_nontemporal_load((const u32x4*)(m + at.m) + i);
+#pragma unroll
+    for (int i = 0; i < (N16 ? 2 : 1); ++i) c.e[i] = e[at.e + i];
 }
 
 // Row of the planes that a stage of 16 tokens (t a multiple of 16, t < len) begins at.  Page numbers come from device memory that the

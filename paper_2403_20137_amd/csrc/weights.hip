@@ -44,6 +44,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     if (place.split >= tiles) return;                            // (uniform for the workgroup)
     const int64_t unit = (int64_t)b * a.H_kv + kvh;
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    const ChunkAt whole = chunk_at<P, N16>(a, l16, group);
 
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
     if (tid < kD) at_s[tid] = tid;                               // (what is no permutation leaves no entry out)
@@ -71,8 +72,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 #pragma unroll
             for (int st = 0; st < kStages; ++st) {
                 const int from = min(t0 + 16 * st, last16);
-                const int off = min(t0 + 16 * st + l16, s.len - 1) - from;
-                load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), off, group, to.raw[st]);
+                ChunkAt at = whole;
+                if (t0 + kWaveTokens > s.len) at = chunk_at<P, N16>(a, min(t0 + 16 * st + l16, s.len - 1) - from, group);
+                load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), at, to.raw[st]);
             }
         };
         request(place.split, next[0]);
