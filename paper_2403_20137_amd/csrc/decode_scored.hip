@@ -82,11 +82,12 @@ constexpr uint32_t kOrdinary = 200;
 struct Running {
     float ref = -INFINITY, most = -INFINITY, sum = 0.f;
 };
-// Takes eight scores (y times factor) into account; returns what they are taken relative to.
-__device__ __forceinline__ float follow(const float (&y)[8], float factor, float slack, Running& x, f32x4 (&o)[8]) {
+// Takes N scores (y times factor) into account; returns what they are taken relative to.
+template <int N>
+__device__ __forceinline__ float follow(const float (&y)[N], float factor, float slack, Running& x, f32x4 (&o)[8]) {
     float top = y[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
+    for (int i = 1; i < N; ++i) top = fmaxf(top, y[i]);
     x.most = fmaxf(x.most, rows_max(top * factor));
     if (__builtin_amdgcn_ballot_w64(x.most > x.ref + slack)) {        // (the reference begins at minus infinity)
         const float f = x.most > -INFINITY ? exp2_raw(x.ref - x.most) : 1.f;
@@ -99,18 +100,21 @@ __device__ __forceinline__ float follow(const float (&y)[8], float factor, float
     }
     return x.ref > -INFINITY ? x.ref : 0.f;
 }
-// Eight scores of a row -> its probabilities as the operand of add_values, and their sum.
-template <int PL>
-__device__ __forceinline__ void probabilities(const float (&y)[8], float factor, float base, float& sum, bf16x8 (&p)[PL]) {
+// N scores of a row -> its probabilities as bf16 pairs, PL of them for each, and their sum.
+template <int PL, int N>
+__device__ __forceinline__ void probabilities(const float (&y)[N], float factor, float base, float& sum, uint32_t (&p)[PL][N / 2]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float w = exp2_raw(fmaf(y[i], factor, -base));
-        sum += w;
-        __bf16 lw[PL];
-        limbs<PL>(w, lw);
-        if (PL == 2) lw[1] = (__bf16)(w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));     // rounded, not cut
+    for (int i = 0; i < N / 2; ++i) {
+        __bf16 l[2][PL];
 #pragma unroll
-        for (int x = 0; x < PL; ++x) p[x][i] = lw[x];
+        for (int h = 0; h < 2; ++h) {
+            const float w = exp2_raw(fmaf(y[2 * i + h], factor, -base));
+            sum += w;
+            limbs<PL>(w, l[h]);
+            if (PL == 2) l[h][1] = (__bf16)(w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));     // rounded, not cut
+        }
+#pragma unroll
+        for (int x = 0; x < PL; ++x) p[x][i] = __builtin_bit_cast(uint32_t, bf16x2{l[0][x], l[1][x]});
     }
 }
 template <int P, bool N16>
@@ -163,10 +167,10 @@ __device__ __forceinline__ void store_partial(const Args& a, int kvh, int r0, in
     for (int ct = 0; ct < 8; ++ct) *(f32x4*)(a.part_o + at * kD + 16 * ct + 4 * group) = o[ct];
     if (group == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(x.ref, sum);
 }
-// The sums of a workgroup's wavefronts for 16 * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
-// 16 (w % RW) ..) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
+// The sums of a workgroup's wavefronts for RP * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
+// 16 (w % RW) .., or twice the same 8 rows, RP = 8, RW = 1) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
 // free when this is called.
-template <int P, int QL, int RW>
+template <int P, int QL, int RW, int RP>
 __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int place, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
                                        const f32x4 (&o)[8], const Running& x) {
     const int tid = threadIdx.x, l16 = lane & 15, group = lane >> 4;
@@ -184,18 +188,24 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
 #pragma unroll
     for (int rw = 0; rw < RW; ++rw) {
         const int r = r0 + 16 * rw + row;
-        if (r >= a.M) continue;
+        if (row >= RP || r >= a.M) continue;
         float top = -INFINITY, den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = rw; w < 4; w += RW) top = fmaxf(top, ml_s[w][row][0]);
+        for (int w = rw; w < 4; w += RW)
+#pragma unroll
+            for (int h = 0; h < 16; h += RP) top = fmaxf(top, ml_s[w][(row + h) & 15][0]);
 #pragma unroll
         for (int w = rw; w < 4; w += RW) {
-            if (!(ml_s[w][row][0] > -INFINITY)) continue;
-            const float f = exp2_raw(ml_s[w][row][0] - top);
-            den = fmaf(f, ml_s[w][row][1], den);
-            const float* const src = (const float*)(smem + w * kWaveLds) + row * kOStride + p0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = fmaf(f, src[i], acc[i]);
+            for (int h = 0; h < 16; h += RP) {
+                const int at = (row + h) & 15;
+                if (!(ml_s[w][at][0] > -INFINITY)) continue;
+                const float f = exp2_raw(ml_s[w][at][0] - top);
+                den = fmaf(f, ml_s[w][at][1], den);
+                const float* const src = (const float*)(smem + w * kWaveLds) + at * kOStride + p0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(f, src[i], acc[i]);
+            }
         }
         if (a.n_splits > 1) {
             const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
@@ -216,9 +226,11 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
     }
 }
 
-// Up to 16 rows: every wavefront has all of them and takes 32 tokens of a tile of 128 for itself.
+// Up to 16 rows: every wavefront has all of them and takes 32 tokens of a tile of 128 for itself.  With up to 8 rows (RP = 8) the 16
+// columns are these rows twice, once for either stage of 16 tokens: each lane then has four scores instead of eight, half of which would
+// be nobody's; the columns are joined in the end like another wavefront's.
 // grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL bf16 numbers of a query.
-template <int P, bool N16, int QL>
+template <int P, bool N16, int QL, int RP>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
     __shared__ __align__(16) uint8_t smem[4 * kWaveLds];
@@ -261,10 +273,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     if (some) request(place.split);
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
     rows.put(a, 0, (float*)smem, perm_s);
-    if (tid < 16) rule_s[tid] = row_rule(a, s, b, kvh, tid);
+    if (tid < RP) rule_s[tid] = row_rule(a, s, b, kvh, tid);
+    const int row = l16 & (RP - 1), mine = RP == 8 ? 16 * (l16 >> 3) : 0;      // its row; where its tokens begin
+    const uint32_t second = l16 & 8 ? ~0u : 0u;
     __syncthreads();
     bf16x8 q[1][QL][4];
-    query_operand<P, QL>((const float*)smem, perm_s, l16, group, q[0]);
+    query_operand<P, QL>((const float*)smem, perm_s, row, group, q[0]);
     __syncthreads();                                         // the queries give way to the values
 
     uint8_t* const v_s = smem + wave * kWaveLds;
@@ -290,15 +304,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1), j & 1)) = eight<P, N16>(vc[st], j);
         if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) slack = 0.f;
         wave_fence();
-        const float factor = rule_scores<8, QL == 3>(a, s, rule_s + l16, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base, t0 + 4 * group, mul, y[0]);
-        const float base = follow(y[0], factor, slack, x[0], o[0]);
+        constexpr int N = RP / 2;
+        float z[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)                          // (by bits: a choice between elements of an array would go through memory)
+            z[i] = RP == 16 ? y[0][i] : __uint_as_float((__float_as_uint(y[0][i & 3]) & ~second) | (__float_as_uint(y[0][4 + (i & 3)]) & second));
+        const float factor = rule_scores<N, QL == 3>(a, s, rule_s + row, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base,
+                                                     t0 + mine + 4 * group, mul, z);
+        const float base = follow<N>(z, factor, slack, x[0], o[0]);
+        uint32_t w[PL][N / 2];
+        probabilities<PL, N>(z, factor, base, x[0].sum, w);
         bf16x8 p[1][PL];
-        probabilities<PL>(y[0], factor, base, x[0].sum, p[0]);
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+            u32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = RP == 16 || ((l16 & 8) != 0) == (k >= 2) ? w[i][k & (N / 2 - 1)] : 0u;
+            p[0][i] = __builtin_bit_cast(bf16x8, v);
+        }
         add_values<PL, 1>(v_s, lane, p, o);
         wave_fence();
     }
     __syncthreads();
-    finish<P, QL, 1>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
+    finish<P, QL, 1, RP>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
 }
 
 // More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
@@ -397,9 +425,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             bf16x8 p[HC][PL];
 #pragma unroll
             for (int c = 0; c < HC; ++c) {
+                uint32_t w[PL][4];
                 const float factor = rule_scores<8, QL == 3>(a, s, rule_s + 16 * (RW * c + rw) + l16, depth_s, inner, t0 + 4 * group, mul, y[c]);
-                const float base = follow(y[c], factor, slack, x[c], o[c]);
-                probabilities<PL>(y[c], factor, base, x[c].sum, p[c]);
+                const float base = follow<8>(y[c], factor, slack, x[c], o[c]);
+                probabilities<PL, 8>(y[c], factor, base, x[c].sum, w);
+#pragma unroll
+                for (int i = 0; i < PL; ++i) p[c][i] = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i][2], w[i][3]});
             }
             add_values<PL, HC>(tile + kPlane + row * 256, lane, p, o);
         }
@@ -411,7 +442,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[c], x[c]);
         } else {
             __syncthreads();
-            if (rc < a.M) finish<P, QL, RW>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
+            if (rc < a.M) finish<P, QL, RW, 16>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
         }
     }
 }
@@ -493,7 +524,8 @@ template <int P, bool N16, int QL>
 void launch_split(const Args& a, const Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)(a.H_kv * a.row_tiles));
     constexpr int kTwo = QL == 1 ? 2 : 1;                    // fp16 and fp32 have no registers for two, and are not planned with them
-    if (p.rw == 1) scored_split<P, N16, QL><<<grid, kThreads, 0, s>>>(a);
+    if (a.M <= 8) scored_split<P, N16, QL, 8><<<grid, kThreads, 0, s>>>(a);
+    else if (p.rw == 1) scored_split<P, N16, QL, 16><<<grid, kThreads, 0, s>>>(a);
     else if (p.rw == 2) scored_split_wide<P, N16, QL, 1, 2><<<grid, kThreads, 0, s>>>(a);
     else if (p.hc == 1) scored_split_wide<P, N16, QL, 1, 4><<<grid, kThreads, 0, s>>>(a);
     else scored_split_wide<P, N16, QL, kTwo, 4><<<grid, kThreads, 0, s>>>(a);
