@@ -58,15 +58,20 @@ __device__ __forceinline__ s16x4 read_by_channel(const uint8_t* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
 }
 
-// o += V^T P^T for 32 tokens and HC times 16 rows: lane (row l % 16): probabilities of tokens 4 (l / 16) .. of either stage.
-template <int PL, int HC>
-__device__ __forceinline__ void add_values(const uint8_t* v_s, int lane, const bf16x8 (&p)[HC][PL], f32x4 (&o)[HC][8]) {
+// Values of 32 tokens by channel: the first operand of the value product for 16 channels each.
+struct Values { bf16x8 v[8]; };
+__device__ __forceinline__ bf16x8 values_of(const uint8_t* v_s, int lane, int ct) {
     const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2), half = (i >> 1) & 1, word = (i & 1) * 8;
+    const s16x4 lo = read_by_channel(v_s + value_at(row, ct, half) + word);
+    const s16x4 hi = read_by_channel(v_s + value_at(row + 16, ct, half) + word);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// o += V^T P^T for 32 tokens and HC times 16 rows: lane (row l % 16): probabilities of tokens 4 (l / 16) .. of either stage.
+template <int PL, int HC, class ByChannel>
+__device__ __forceinline__ void add_values(ByChannel&& values, const bf16x8 (&p)[HC][PL], f32x4 (&o)[HC][8]) {
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) {
-        const s16x4 lo = read_by_channel(v_s + value_at(row, ct, half) + word);
-        const s16x4 hi = read_by_channel(v_s + value_at(row + 16, ct, half) + word);
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        const bf16x8 v = values(ct);
 #pragma unroll
         for (int c = 0; c < HC; ++c)
 #pragma unroll
@@ -276,10 +281,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     if (tid < RP) rule_s[tid] = row_rule(a, s, b, kvh, tid);
     const int row = l16 & (RP - 1), mine = RP == 8 ? 16 * (l16 >> 3) : 0;      // its row; where its tokens begin
     const uint32_t second = l16 & 8 ? ~0u : 0u;
-    __syncthreads();
+    lds_only_barrier();                                      // (the first rows are on their way)
     bf16x8 q[1][QL][4];
     query_operand<P, QL>((const float*)smem, perm_s, row, group, q[0]);
-    __syncthreads();                                         // the queries give way to the values
+    lds_only_barrier();                                      // the queries give way to the values
 
     uint8_t* const v_s = smem + wave * kWaveLds;
     f32x4 o[1][8];
@@ -322,7 +327,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             for (int k = 0; k < 4; ++k) v[k] = RP == 16 || ((l16 & 8) != 0) == (k >= 2) ? w[i][k & (N / 2 - 1)] : 0u;
             p[0][i] = __builtin_bit_cast(bf16x8, v);
         }
-        add_values<PL, 1>(v_s, lane, p, o);
+        add_values<PL, 1>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
         wave_fence();
     }
     __syncthreads();
@@ -378,12 +383,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     bf16x8 q[HC][QL][4];
 #pragma unroll
     for (int c = 0; c < HC; ++c) {
-        if (c > 0) __syncthreads();
+        if (c > 0) lds_only_barrier();
         rows[c].put(a, r0 + 16 * RW * c, (float*)smem, perm_s);
-        __syncthreads();
+        lds_only_barrier();                                  // (the first rows are on their way)
         query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[c]);
     }
-    __syncthreads();                                         // the queries give way to keys and values
+    lds_only_barrier();                                      // the queries give way to keys and values
 
     f32x4 o[HC][8];
     Running x[HC];
@@ -410,17 +415,36 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     int half = 0;
     float slack = kSlack;
     for (int v = place.split; v < tiles.count; v += n_splits, half ^= 1) {
-        __syncthreads();                                     // this tile is complete; the one before it is not looked at any more
+        lds_only_barrier();                                  // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
         if (v + n_splits < tiles.count) decode(half ^ 1);
         request(after(after(v)));
         if (large_s[half]) slack = 0.f;
-        // (32 tokens at a time, not unrolled: the registers of two steps together do not fit)
+        // 32 tokens at a time, not unrolled: the registers of two steps together do not fit.  With 16 rows a wavefront the values and the
+        // next keys are read ahead of the softmax, whose instructions then fill the time of the reads.
+        bf16x8 k[2][4];
+        auto read_keys = [&](int row) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[st][j] = *(const bf16x8*)(tile + key_at(row + 16 * st + l16, 4 * group + j));
+        };
+        if (HC == 1) read_keys(32 * KS * part);
 #pragma unroll 1
         for (int ks = 0; ks < KS; ++ks) {
             const int row = 32 * (KS * part + ks), t0 = tiles.at(v) * kWideTokens + row;
+            const uint8_t* const v_s = tile + kPlane + row * 256;
             float y[HC][8];
-            products<QL, HC>([&](int st, int j) { return *(const bf16x8*)(tile + key_at(row + 16 * st + l16, 4 * group + j)); }, q, y);
+            Values by_channel;
+            if (HC == 1) {
+                products<QL, HC>([&](int st, int j) { return k[st][j]; }, q, y);
+#pragma unroll
+                for (int ct = 0; ct < 8; ++ct) by_channel.v[ct] = values_of(v_s, lane, ct);
+                if (ks + 1 < KS) read_keys(row + 32);
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                products<QL, HC>([&](int st, int j) { return *(const bf16x8*)(tile + key_at(row + 16 * st + l16, 4 * group + j)); }, q, y);
+            }
             const bool inner = t0 >= lo_most && t0 + 32 <= s.base;
             bf16x8 p[HC][PL];
 #pragma unroll
@@ -432,7 +456,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int i = 0; i < PL; ++i) p[c][i] = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i][2], w[i][3]});
             }
-            add_values<PL, HC>(tile + kPlane + row * 256, lane, p, o);
+            if (HC == 1) add_values<PL, HC>([&](int ct) { return by_channel.v[ct]; }, p, o);
+            else add_values<PL, HC>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
         }
     }
 #pragma unroll
