@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     const int b = place.b, kvh = blockIdx.y, n_splits = place.n;
     QueryRows<QL, 16> rows;
     rows.request(a, b, kvh, 0);
-    const Seq s = sequence(a, b);
+    const Seq s = sequence(a, b, place.len);
     int lo_least, lo_most;
     row_limits(a, s, b, 0, 16, lo_least, lo_most);
     const auto tiles = tiles_of<kTileTokens>(s, lo_least);
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     QueryRows<QL, 16 * RW> rows[HC];
 #pragma unroll
     for (int c = 0; c < HC; ++c) rows[c].request(a, b, kvh, r0 + 16 * RW * c);
-    const Seq s = sequence(a, b);
+    const Seq s = sequence(a, b, place.len);
     int lo_least, lo_most;
     row_limits(a, s, b, r0, 16 * RW * HC, lo_least, lo_most);
     const auto tiles = tiles_of<kWideTokens>(s, lo_least);
@@ -445,6 +445,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             } else {
                 products<QL, HC>([&](int st, int j) { return *(const bf16x8*)(tile + key_at(row + 16 * st + l16, 4 * group + j)); }, q, y);
             }
+            __builtin_amdgcn_s_setprio(0);
             const bool inner = t0 >= lo_most && t0 + 32 <= s.base;
             bf16x8 p[HC][PL];
 #pragma unroll
@@ -456,6 +457,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int i = 0; i < PL; ++i) p[c][i] = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i][2], w[i][3]});
             }
+            __builtin_amdgcn_s_setprio(1);
             if (HC == 1) add_values<PL, HC>([&](int ct) { return by_channel.v[ct]; }, p, o);
             else add_values<PL, HC>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
         }
@@ -472,77 +474,95 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 }
 
-// Joins the splits: WPR wavefronts per row (1 or 4, which take every fourth split), two channels a lane, sixteen partial results in flight.
-template <int P, int QL, int WPR>
+// Joins the splits, two channels a lane, sixteen partial results in flight: four wavefronts for a row, which take every fourth split (FOUR),
+// or one for four rows of a kv-head, four splits of each at a time.
+template <int P, int QL, bool FOUR>
 __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
     __shared__ float join_s[4][64][4];
-    constexpr int kFly = 16;
+    constexpr int kRows = FOUR ? 1 : 4, kFly = 16 / kRows, kStep = FOUR ? 4 : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + wave / WPR;          // (b * H_kv + kvh) * M + r
-    if (row >= (int64_t)a.batch * a.H_kv * a.M) return;
-    const int unit = (int)(row / a.M), r = (int)(row - (int64_t)unit * a.M), b = unit / a.H_kv, kvh = unit - b * a.H_kv;
+    const int tiles = (a.M + kRows - 1) / kRows;               // of rows, per kv-head
+    const int64_t tile = FOUR ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+    if (tile >= (int64_t)a.batch * a.H_kv * tiles) return;     // (uniform for the workgroup where it has a barrier)
+    const int unit = (int)(tile / tiles), r0 = (int)(tile - (int64_t)unit * tiles) * kRows, b = unit / a.H_kv, kvh = unit - b * a.H_kv;
     const Place place = places_of(a, b);
-    const int64_t first = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place.first;
     int c0 = position_channel<P>(2 * lane), c1 = position_channel<P>(2 * lane + 1);
     if (a.perm_v) {
         c0 = a.perm_v[kvh * kD + c0] & (kD - 1);
         c1 = a.perm_v[kvh * kD + c1] & (kD - 1);
     }
-    float top = -INFINITY, den = 0.f;
-    float2 acc = {0.f, 0.f};
-    const int part = wave % WPR;
-    for (int i0 = part; i0 < place.n; i0 += kFly * WPR) {
-        float2 v[kFly];
-        const int mine = i0 + (lane & (kFly - 1)) * WPR;
-        float2 ml = *(const float2*)(a.part_ml + 2 * (first + min(mine, place.n - 1)));
-        if (mine >= place.n) ml.x = -INFINITY;
+    float top[kRows], den[kRows];
+    float2 acc[kRows];
+    int64_t first[kRows];
 #pragma unroll
-        for (int i = 0; i < kFly; ++i)
-            if (i0 + i * WPR < place.n) v[i] = *(const float2*)(a.part_o + (first + i0 + i * WPR) * kD + 2 * lane);      // (uniform)
-        float now = fmaxf(top, row_max(ml.x));
-        const float ref = now > -INFINITY ? now : 0.f;
-        const float w = exp2_raw(ml.x - ref), was = exp2_raw(top - ref);       // 0 for a split that saw nothing
-        top = now;
-        den = fmaf(den, was, row_sum(w * ml.y));
-        acc.x *= was;
-        acc.y *= was;
+    for (int k = 0; k < kRows; ++k) {
+        top[k] = -INFINITY;
+        den[k] = acc[k].x = acc[k].y = 0.f;
+        first[k] = ((int64_t)kvh * a.M + min(r0 + k, a.M - 1)) * a.n_splits * a.batch + place.first;
+    }
+    const int part = FOUR ? wave : 0;
+    for (int i0 = part; i0 < place.n; i0 += kFly * kStep) {
+        float2 v[kRows][kFly], ml[kRows];
+        const int mine = i0 + (lane & (kFly - 1)) * kStep;
 #pragma unroll
-        for (int i = 0; i < kFly; ++i) {
-            if (i0 + i * WPR < place.n) {
+        for (int k = 0; k < kRows; ++k) ml[k] = *(const float2*)(a.part_ml + 2 * (first[k] + min(mine, place.n - 1)));
+#pragma unroll
+        for (int k = 0; k < kRows; ++k)
+#pragma unroll
+            for (int i = 0; i < kFly; ++i)
+                if (i == 0 || i0 + i * kStep < place.n) v[k][i] = *(const float2*)(a.part_o + (first[k] + i0 + i * kStep) * kD + 2 * lane);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            if (mine >= place.n) ml[k].x = -INFINITY;
+            const float now = fmaxf(top[k], row_max(ml[k].x));
+            const float ref = now > -INFINITY ? now : 0.f;
+            const float w = exp2_raw(ml[k].x - ref), was = exp2_raw(top[k] - ref);       // 0 for a split that saw nothing
+            top[k] = now;
+            acc[k].x *= was;
+            acc[k].y *= was;
+            den[k] *= was;
+#pragma unroll
+            for (int i = 0; i < kFly; ++i) {
+                if (i > 0 && i0 + i * kStep >= place.n) break;                           // (not by a weight of 0)
                 const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
-                acc.x = fmaf(wi, v[i].x, acc.x);
-                acc.y = fmaf(wi, v[i].y, acc.y);
+                acc[k].x = fmaf(wi, v[k][i].x, acc[k].x);
+                acc[k].y = fmaf(wi, v[k][i].y, acc[k].y);
+                den[k] = fmaf(wi, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ml[k].y), i)), den[k]);
             }
         }
     }
-    if (WPR > 1) {
-        *(f32x4*)join_s[wave][lane] = f32x4{top, den, acc.x, acc.y};
+    if (FOUR) {
+        *(f32x4*)join_s[wave][lane] = f32x4{top[0], den[0], acc[0].x, acc[0].y};
         __syncthreads();
         if (part) return;
         float all = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) all = fmaxf(all, join_s[w][lane][0]);
+        for (int w = 0; w < 4; ++w) all = fmaxf(all, join_s[w][lane][0]);
         const float ref = all > -INFINITY ? all : 0.f;
-        top = all;
-        den = acc.x = acc.y = 0.f;
+        top[0] = all;
+        den[0] = acc[0].x = acc[0].y = 0.f;
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) {
+        for (int w = 0; w < 4; ++w) {
             const f32x4 x = *(const f32x4*)join_s[w][lane];
             const float f = exp2_raw(x[0] - ref);
-            den = fmaf(f, x[1], den);
-            acc.x = fmaf(f, x[2], acc.x);
-            acc.y = fmaf(f, x[3], acc.y);
+            den[0] = fmaf(f, x[1], den[0]);
+            acc[0].x = fmaf(f, x[2], acc[0].x);
+            acc[0].y = fmaf(f, x[3], acc[0].y);
         }
     }
-    const float by = den > 0.f ? (float)(1 << Decode<P>::kShift) / den : 0.f;
-    const int64_t at = out_row(a, b, kvh, r);
-    store_out<QL>(a, at * kD + c0, acc.x * by);
-    store_out<QL>(a, at * kD + c1, acc.y * by);
-    if (lane == 0 && a.lse) a.lse[at] = natural_lse(top, den);
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        if (r0 + k >= a.M) break;
+        const float by = den[k] > 0.f ? (float)(1 << Decode<P>::kShift) / den[k] : 0.f;
+        const int64_t at = out_row(a, b, kvh, r0 + k);
+        store_out<QL>(a, at * kD + c0, acc[k].x * by);
+        store_out<QL>(a, at * kD + c1, acc[k].y * by);
+        if (lane == 0 && a.lse) a.lse[at] = natural_lse(top[k], den[k]);
+    }
 }
 
-// Rows of a workgroup: 16 in scored_split (rw = 1), 16 * rw * hc in scored_split_wide; splits: enough workgroups for the compute units, and
-// no more than there are tiles.
+// Rows of a workgroup: 16 in scored_split (rw = 1), 16 * rw * hc in scored_split_wide; splits: as many as make one resident round of
+// workgroups (three a compute unit in scored_split, two in scored_split_wide), and no more than there are tiles.
 struct Plan { int32_t hc, rw, row_tiles, n_splits; };
 
 template <int P, bool N16, int QL>
@@ -566,12 +586,13 @@ void launch_split(const Args& a, int dt, const Plan& p, hipStream_t s) {
     else launch_split<P, false, 1>(a, p, s);
 }
 
-// Few rows with many splits: four wavefronts for each.
+// Few rows: four wavefronts for each.
 template <int P, int QL>
 void launch_combine(const Args& a, hipStream_t s) {
     const int64_t rows = (int64_t)a.batch * a.H_kv * a.M;
-    if (a.n_splits > 4 && rows <= 2048) scored_combine<P, QL, 4><<<dim3((unsigned)rows), kThreads, 0, s>>>(a);
-    else scored_combine<P, QL, 1><<<dim3((unsigned)((rows + 3) / 4)), kThreads, 0, s>>>(a);
+    const int64_t tiles = (int64_t)a.batch * a.H_kv * ((a.M + 3) / 4);
+    if (rows <= 2048) scored_combine<P, QL, true><<<dim3((unsigned)rows), kThreads, 0, s>>>(a);
+    else scored_combine<P, QL, false><<<dim3((unsigned)((tiles + 3) / 4)), kThreads, 0, s>>>(a);
 }
 template <int P>
 void launch_combine(const Args& a, int dt, hipStream_t s) {
@@ -580,13 +601,13 @@ void launch_combine(const Args& a, int dt, hipStream_t s) {
     else launch_combine<P, 1>(a, s);
 }
 
-// The splits, and with them the workspace, do not depend on the type.
+// The most splits that a call takes; the workspace, which does not depend on the type, has room for them.
 int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
     const int64_t of_wg = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     const int64_t units = (int64_t)L->batch * L->n_kv_heads * ((rows + of_wg - 1) / of_wg);
     const int64_t tile = rows > 16 ? kWideTokens : kTileTokens, tiles = (max_len + tile - 1) / tile;
     const int64_t wanted = rows <= 16 ? 768 : 512;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (wanted + units - 1) / units));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, wanted / units));
 }
 Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
     Plan p;
@@ -594,7 +615,10 @@ Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
     p.rw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t of_wg = 16 * p.hc * p.rw;
     p.row_tiles = (int32_t)((rows + of_wg - 1) / of_wg);
+    // (fp16 and fp32 have more, smaller workgroups: one resident round all the same)
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads * p.row_tiles;
     p.n_splits = splits_of(L, rows, max_len);
+    if (p.rw > 1) p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.n_splits, 512 / units));
     return p;
 }
 

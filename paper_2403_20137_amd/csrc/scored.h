@@ -55,10 +55,9 @@ struct Args {
 struct Seq {
     int32_t len, base, prefix;           // tokens [base, len) are the last n_tok; base may be negative
 };
-__device__ __forceinline__ Seq sequence(const Args& a, int b) {
+__device__ __forceinline__ Seq sequence(const Args& a, int b, int len) {
     Seq s;
-    s.len = a.max_len;
-    if (a.seq_len) s.len = min(max(a.seq_len[b], 0), a.max_len);
+    s.len = len;
     s.base = s.len - a.n_tok;
     s.prefix = a.prefix ? min(max(a.prefix[b], 0), s.len) : 0;
     return s;
@@ -67,7 +66,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
 // Which part of which sequence a place takes: part `split` of `n`, the places of the sequence begin at `first`.  Equal parts
 // (n_splits each), or shared out by what the sequences have to read (up to 64 of them, a lane each): one each, the others in
 // proportion, rounded down, what is left by the largest remainders.
-struct Place { int b, split, n, first; };
+struct Place { int b, split, n, first, len; };
 // Inclusive sum over the lanes of a wavefront: within the rows of 16 by shifts, then the rows' last sums into the rows behind them.  (Six
 // exchanges through LDS take six times its latency; 0 for a lane that nothing comes to.)
 template <int CTRL, int ROWS>
@@ -91,16 +90,13 @@ __device__ __forceinline__ float wave_scan(float v) {
     v += step(dpp_or_zero<0x143, 0xC>(__float_as_int(v)));
     return v;
 }
-__device__ __forceinline__ int tokens_read(const Args& a, int b) {        // about: documents are not looked at
-    int len = min(max(a.seq_len[b], 0), a.max_len);
-    if (a.window) {
-        const int near = a.window + a.n_tok + (a.prefix ? min(max(a.prefix[b], 0), len) : 0);
-        len = min(len, near);
-    }
-    return len;
-}
-__device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first) {
-    const float mine = lane < a.batch ? (float)(tokens_read(a, lane) + 1) : 0.f;
+__device__ __forceinline__ int length_of(const Args& a, int b) { return a.seq_len ? min(max(a.seq_len[b], 0), a.max_len) : a.max_len; }
+// Lane b: the places of sequence b, the first of them, its length.
+__device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first, int& len) {
+    len = length_of(a, min(lane, a.batch - 1));
+    int read = len;                      // about what there is to read: documents are not looked at
+    if (a.window) read = min(len, a.window + a.n_tok + (a.prefix ? min(max(a.prefix[min(lane, a.batch - 1)], 0), len) : 0));
+    const float mine = lane < a.batch ? (float)(read + 1) : 0.f;
     const float all = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wave_scan(mine)), 63));
     const float extra = (float)((a.n_splits - 1) * a.batch);
     const float share = extra * (mine / all) * (1.f + 0x1p-20f);         // (a whole number stays one)
@@ -124,25 +120,26 @@ __device__ __forceinline__ Place place_at(const Args& a, int at) {
         p.split = at - p.b * a.n_splits;
         p.n = a.n_splits;
         p.first = at - p.split;
+        p.len = length_of(a, p.b);
         return p;
     }
-    const int lane = threadIdx.x & 63;
-    int n, first;
-    share_places(a, lane, n, first);
+    int n, first, len;
+    share_places(a, threadIdx.x & 63, n, first, len);
     const uint64_t found = __ballot(at >= first && at < first + n);
     const int who = found ? __ffsll((unsigned long long)found) - 1 : 0;
     p.b = __builtin_amdgcn_readfirstlane(who);
     p.n = __builtin_amdgcn_readlane(n, p.b);
     p.first = __builtin_amdgcn_readlane(first, p.b);
+    p.len = __builtin_amdgcn_readlane(len, p.b);
     p.split = found ? at - p.first : -1;
     return p;
 }
 // The places of sequence b.
 __device__ __forceinline__ Place places_of(const Args& a, int b) {
-    Place p = {b, 0, a.n_splits, b * a.n_splits};
+    Place p = {b, 0, a.n_splits, b * a.n_splits, 0};
     if (a.share) {
-        int n, first;
-        share_places(a, threadIdx.x & 63, n, first);
+        int n, first, len;
+        share_places(a, threadIdx.x & 63, n, first, len);
         p.n = __builtin_amdgcn_readlane(n, b);
         p.first = __builtin_amdgcn_readlane(first, b);
     }

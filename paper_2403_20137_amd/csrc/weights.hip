@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     const Place place = place_at(a, blockIdx.x);
     if (place.split < 0) return;
     const int b = place.b, kvh = blockIdx.y;
-    const Seq s = sequence(a, b);
+    const Seq s = sequence(a, b, place.len);
     const int tiles = (s.len + kTileTokens - 1) / kTileTokens, last16 = (s.len - 1) & ~15;
     if (place.split >= tiles) return;                            // (uniform for the workgroup)
     const int64_t unit = (int64_t)b * a.H_kv + kvh;
