@@ -54,6 +54,30 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
+// Inclusive sum over the lanes of a wavefront: within the rows of 16 by shifts, then the rows' last sums into the rows behind them.  (Six
+// exchanges through LDS take six times its latency; 0 for a lane that nothing comes to.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    v += dpp_or_zero<0x143, 0xC>(v);
+    return v;
+}
+__device__ __forceinline__ float wave_scan(float v) {
+    auto step = [](int x) { return __int_as_float(x); };
+    v += step(dpp_or_zero<0x111, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x112, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x114, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x118, 0xF>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x142, 0xA>(__float_as_int(v)));
+    v += step(dpp_or_zero<0x143, 0xC>(__float_as_int(v)));
+    return v;
+}
+
 __device__ __forceinline__ float load_as_float(const void* p, int dt, int64_t i) {
     if (dt == KVBFP_F32) return ((const float*)p)[i];
     const uint32_t h = ((const uint16_t*)p)[i];

@@ -602,14 +602,14 @@ void launch_combine(const Args& a, int dt, hipStream_t s) {
 }
 
 // The most splits that a call takes; the workspace, which does not depend on the type, has room for them.
-int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
+int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len, bool shares) {
     const int64_t of_wg = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     const int64_t units = (int64_t)L->batch * L->n_kv_heads * ((rows + of_wg - 1) / of_wg);
     const int64_t tile = rows > 16 ? kWideTokens : kTileTokens, tiles = (max_len + tile - 1) / tile;
     const int64_t wanted = rows <= 16 ? 768 : 512;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, wanted / units));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, round_of(wanted, units, shares)));
 }
-Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
+Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype, bool shares) {
     Plan p;
     p.hc = rows > 64 && dtype == KVBFP_BF16 ? 2 : 1;
     p.rw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
@@ -617,8 +617,8 @@ Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype) {
     p.row_tiles = (int32_t)((rows + of_wg - 1) / of_wg);
     // (fp16 and fp32 have more, smaller workgroups: one resident round all the same)
     const int64_t units = (int64_t)L->batch * L->n_kv_heads * p.row_tiles;
-    p.n_splits = splits_of(L, rows, max_len);
-    if (p.rw > 1) p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.n_splits, 512 / units));
+    p.n_splits = splits_of(L, rows, max_len, shares);
+    if (p.rw > 1) p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.n_splits, round_of(512, units, shares)));
     return p;
 }
 
@@ -704,7 +704,8 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
         return rc;
     if (!out) return fail(KVBFP_ERR_INVALID_ARG, "%s: out is NULL", call);
     if ((uintptr_t)out % dtype_size(dtype) != 0) return fail(KVBFP_ERR_INVALID_ARG, "%s: out is not aligned to its elements", call);
-    const Plan p = plan(&logical, a.M, max_len, (int)dtype);
+    const bool shares = seq_len_dev && a.batch > 1 && a.batch <= 64;
+    const Plan p = plan(&logical, a.M, max_len, (int)dtype, shares);
     if ((int64_t)a.H_kv * p.row_tiles > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     const size_t need = partial_bytes(&logical, a.M, p.n_splits);
     if (need && (!workspace || workspace_bytes < need))
@@ -712,7 +713,7 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
     if (need && (uintptr_t)workspace % 256 != 0) return fail(KVBFP_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", call);
     a.out = out; a.lse = lse; a.perm_k = perm_k; a.perm_v = perm_v;
     a.n_splits = p.n_splits; a.row_tiles = p.row_tiles;
-    a.share = seq_len_dev && a.batch > 1 && a.batch <= 64 && p.n_splits > 1;
+    a.share = shares && p.n_splits > 1;
     if (need) {
         a.part_o = (float*)workspace;
         a.part_ml = a.part_o + (size_t)a.batch * a.H_kv * a.M * a.n_splits * kD;
@@ -740,7 +741,7 @@ size_t kvbfp_scored_workspace_bytes(const kvbfp_layout* L, int32_t n_q_heads, in
         return 0;
     }
     const int64_t rows = (int64_t)(n_q_heads / L->n_kv_heads) * n_q_tokens;
-    return std::max<size_t>(partial_bytes(L, rows, splits_of(L, rows, max_len)), 256);
+    return std::max<size_t>(partial_bytes(L, rows, splits_of(L, rows, max_len, true)), 256);
 }
 
 size_t kvbfp_scored_workspace_bytes_paged(const kvbfp_layout* pool, int64_t table_stride, int32_t batch, int32_t n_q_heads,

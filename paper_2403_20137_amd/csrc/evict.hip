@@ -11,11 +11,14 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "decode_dev.h"
 #include "kvbfp_internal.h"
 
 namespace {
 
-constexpr int kD = 128;
+using kvbfp::dev::kD;
+using kvbfp::dev::wave_scan;
+
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 
@@ -145,12 +148,7 @@ __global__ __launch_bounds__(kThreads) void evict_select(EvictArgs a) {
         mine.x += odd.x;
         mine.y += odd.y;
         const int total = mine.x + mine.y;
-        int before = total;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(before, d);
-            if (lane >= d) before += up;
-        }
+        int before = wave_scan(total);
         if (lane == 63) wave_s[wave][0] = before;
         __syncthreads();
         before -= total;

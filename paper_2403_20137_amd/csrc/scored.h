@@ -67,29 +67,9 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b, int len) {
 // (n_splits each), or shared out by what the sequences have to read (up to 64 of them, a lane each): one each, the others in
 // proportion, rounded down, what is left by the largest remainders.
 struct Place { int b, split, n, first, len; };
-// Inclusive sum over the lanes of a wavefront: within the rows of 16 by shifts, then the rows' last sums into the rows behind them.  (Six
-// exchanges through LDS take six times its latency; 0 for a lane that nothing comes to.)
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
-__device__ __forceinline__ int wave_scan(int v) {
-    v += dpp_or_zero<0x111, 0xF>(v);
-    v += dpp_or_zero<0x112, 0xF>(v);
-    v += dpp_or_zero<0x114, 0xF>(v);
-    v += dpp_or_zero<0x118, 0xF>(v);
-    v += dpp_or_zero<0x142, 0xA>(v);
-    v += dpp_or_zero<0x143, 0xC>(v);
-    return v;
-}
-__device__ __forceinline__ float wave_scan(float v) {
-    auto step = [](int x) { return __int_as_float(x); };
-    v += step(dpp_or_zero<0x111, 0xF>(__float_as_int(v)));
-    v += step(dpp_or_zero<0x112, 0xF>(__float_as_int(v)));
-    v += step(dpp_or_zero<0x114, 0xF>(__float_as_int(v)));
-    v += step(dpp_or_zero<0x118, 0xF>(__float_as_int(v)));
-    v += step(dpp_or_zero<0x142, 0xA>(__float_as_int(v)));
-    v += step(dpp_or_zero<0x143, 0xC>(__float_as_int(v)));
-    return v;
-}
+// Splits of each sequence and head that fill one resident round of workgroups; two where they are shared out by lengths and more than one
+// fits: with one split the longest sequence is one workgroup's.
+inline int64_t round_of(int64_t round, int64_t units, bool shares) { return round / units == 1 && shares && round > units ? 2 : round / units; }
 __device__ __forceinline__ int length_of(const Args& a, int b) { return a.seq_len ? min(max(a.seq_len[b], 0), a.max_len) : a.max_len; }
 // Lane b: the places of sequence b, the first of them, its length.
 __device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first, int& len) {

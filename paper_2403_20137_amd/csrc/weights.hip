@@ -21,19 +21,83 @@ using namespace kvbfp::scored;
 constexpr int kThreads = 256;
 constexpr int kStages = 2;                       // of 16 tokens, per wavefront
 constexpr int kWaveTokens = 16 * kStages;
-constexpr int kTileTokens = 4 * kWaveTokens;
 
-// grid = (n_splits * B, H_kv); QL bf16 numbers of a query
-template <int P, bool N16, int QL>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void accumulate_weights(Args a) {
+// ROWS query rows from r0 on (zeros behind the last row of the kv-head) on their way to LDS as matrix operands: QL planes of bf16 numbers, a row
+// 256 bytes in the order of eight(), its 16-byte pieces exchanged by the row's number.  Called by the whole workgroup of 256: request(), which
+// asks for the first 16 EARLY rows, place(), a barrier, put(), a barrier, staged_operand().  A thread has the same eight channels of every
+// sixteenth row, so where they go is worked out once.
+template <int P, int QL, int ROWS, int EARLY>
+struct StagedRows {
     typedef typename Io<QL>::T T;
     typedef T Tx8 __attribute__((ext_vector_type(8)));
+    Tx8 first[EARLY];
+    int channel;                         // of the query, that belongs at position tid
+    __device__ __forceinline__ Tx8 load(const Args& a, int b, int kvh, int r0) const {
+        const int r = min(r0 + (threadIdx.x >> 4), a.M - 1), tok = r / a.G;
+        const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + (threadIdx.x & 15) * 8;
+        Tx8 x;
+        if (((uintptr_t)a.q & 15u) == 0) {
+            x = *(const Tx8*)src;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = src[k];
+        }
+        return x;
+    }
+    __device__ __forceinline__ void request(const Args& a, int b, int kvh, int r0) {
+        const int cached = position_channel<P>(threadIdx.x & (kD - 1));
+        channel = a.perm_k ? a.perm_k[kvh * kD + cached] & (kD - 1) : cached;                     // masked: stays inside the row
+#pragma unroll
+        for (int p = 0; p < EARLY; ++p) {
+            if (p > 0 && r0 + 16 * p >= a.M) break;
+            first[p] = load(a, b, kvh, r0 + 16 * p);
+        }
+    }
+    __device__ __forceinline__ void place(int* at_s) const {
+        if (threadIdx.x < kD) at_s[channel] = threadIdx.x;
+    }
+    __device__ __forceinline__ void put(const Args& a, int b, int kvh, int r0, uint8_t* q_s, const int* at_s) const {
+        const int row = threadIdx.x >> 4, c = (threadIdx.x & 15) * 8;
+        int to[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int at = at_s[c + k] & (kD - 1);           // (masked: what is no permutation leaves entries out)
+            to[k] = row * 256 + (((at >> 3) ^ row) * 16) + (at & 7) * 2;
+        }
+        auto put16 = [&](int p, const Tx8& x) {
+            const bool there = r0 + row + 16 * p < a.M;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                __bf16 l[QL];
+                limbs<QL>((float)x[k], l);
+#pragma unroll
+                for (int n = 0; n < QL; ++n) *(uint16_t*)(q_s + n * (ROWS * 256) + p * (16 * 256) + to[k]) = there ? __builtin_bit_cast(unsigned short, l[n]) : 0;
+            }
+        };
+#pragma unroll
+        for (int p = 0; p < EARLY; ++p)
+            if (p == 0 || r0 + 16 * p < a.M) put16(p, first[p]);
+        for (int p = EARLY; p < ROWS / 16 && r0 + 16 * p < a.M; ++p) put16(p, load(a, b, kvh, r0 + 16 * p));
+    }
+};
+// The operand of 16 rows from r0 on (a multiple of 16): lane (row l % 16, group l / 16), step j: channels 32 group + 8 j .. in the order of eight().
+template <int ROWS>
+__device__ __forceinline__ bf16x8 staged_operand(const uint8_t* q_s, int n, int r0, int l16, int group, int j) {
+    return *(const bf16x8*)(q_s + n * (ROWS * 256) + (r0 + l16) * 256 + (((4 * group + j) ^ l16) * 16));
+}
+
+// grid = (n_splits * B, H_kv); QL bf16 numbers of a query.  SHARED: the four wavefronts have the same 32 tokens and every fourth 16 rows, and
+// add up in LDS, where there are too few tokens for a resident round of workgroups that have 32 for each wavefront.
+template <int P, bool N16, int QL, bool SHARED>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void accumulate_weights(Args a) {
     constexpr int kChunk = QL == 3 ? 64 : 128;                   // rows in LDS
-    __shared__ __align__(16) uint8_t q_s[QL][kChunk * 256];      // rows in the order of eight(), 16-byte pieces exchanged by the row
+    constexpr int kTileTokens = SHARED ? kWaveTokens : 4 * kWaveTokens, kStep = SHARED ? 4 : 1;
+    __shared__ __align__(16) uint8_t q_s[QL * kChunk * 256];
     __shared__ RowRule rule_s[kChunk];
     __shared__ float ref_s[kChunk];                              // -lse in base 2; minus infinity: the row has no weights to give
     __shared__ int at_s[kD];                                     // position of a channel of the query
     __shared__ int depth_s[64];
+    __shared__ float sum_s[2][4][kWaveTokens];                   // SHARED: in turns
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, group = lane >> 4;
     const Place place = place_at(a, blockIdx.x);
@@ -47,13 +111,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     const ChunkAt whole = chunk_at<P, N16>(a, l16, group);
 
     if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
-    if (tid < kD) at_s[tid] = tid;                               // (what is no permutation leaves no entry out)
-    __syncthreads();
-    if (tid < kD) {
-        const int channel = position_channel<P>(tid);
-        at_s[a.perm_k ? a.perm_k[kvh * kD + channel] & (kD - 1) : channel] = tid;
-    }
     for (int r0 = 0; r0 < a.M; r0 += kChunk) {
+        StagedRows<P, QL, kChunk, SHARED ? (QL == 3 ? 2 : 4) : 1> queries;
+        queries.request(a, b, kvh, r0);
         int lo_least, lo_most;
         row_limits(a, s, b, r0, kChunk, lo_least, lo_most);
         struct Tile {
@@ -65,7 +125,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         // those that no row sees stand for something that is read anyway.)
         auto request = [&](int v, Tile& to) {
             v = min(v, tiles - 1);
-            int t0 = v * kTileTokens + wave * kWaveTokens;
+            int t0 = v * kTileTokens + (SHARED ? 0 : wave) * kWaveTokens;
             const int64_t mine = unit * a.w_stride + min(t0 + min(lane, kWaveTokens - 1), s.len - 1);
             to.before = *(r0 > 0 ? a.w_out + mine : a.w_in ? a.w_in + mine : a.lse_in);
             t0 = sees(t0) ? t0 : last16;
@@ -79,28 +139,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         };
         request(place.split, next[0]);
         request(place.split + place.n, next[1]);
-        __syncthreads();                                         // at_s is complete; nobody looks at the rows before these any more
+        queries.place(at_s);
+        lds_only_barrier();                                      // at_s is complete; nobody looks at the rows before these any more
         const int rows = min(a.M - r0, kChunk), groups = (rows + 15) / 16;
-        const bool vec = ((uintptr_t)a.q & 15u) == 0;
-        for (int i = tid; i < groups * 256; i += kThreads) {
-            const int row = i >> 4, c = (i & 15) * 8, r = min(r0 + row, a.M - 1), tok = r / a.G;
-            const T* const src = (const T*)a.q + (((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)) * kD + c;
-            Tx8 x;
-            if (vec) {
-                x = *(const Tx8*)src;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = src[k];
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                __bf16 l[QL];
-                limbs<QL>((float)x[k], l);
-                const int p = at_s[c + k];
-#pragma unroll
-                for (int n = 0; n < QL; ++n) *(__bf16*)(q_s[n] + row * 256 + (((p >> 3) ^ (row & 15)) * 16) + (p & 7) * 2) = l[n];
-            }
-        }
+        queries.put(a, b, kvh, r0, q_s, at_s);
         if (tid < kChunk) {
             const int r = r0 + tid;
             rule_s[tid] = row_rule(a, s, b, kvh, r);
@@ -112,9 +154,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             }
             ref_s[tid] = ref;
         }
-        __syncthreads();
+        lds_only_barrier();
         auto step = [&](int v, Tile& from) {
-            const int t0 = v * kTileTokens + wave * kWaveTokens;
+            const int t0 = v * kTileTokens + (SHARED ? 0 : wave) * kWaveTokens;
             if (t0 >= s.len) return;
             float* const w_out = a.w_out + unit * a.w_stride + t0 + lane;
             const bool mine = lane < kWaveTokens && t0 + lane < s.len;
@@ -129,7 +171,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                     for (int j = 0; j < 4; ++j) k[st][j] = __builtin_bit_cast(bf16x8, eight<P, N16>(from.raw[st], j));
             }
             request(v + 2 * place.n, from);
-            for (int g = 0; seen && g < groups; ++g) {
+            for (int g = SHARED ? wave : 0; seen && g < groups; g += kStep) {
                 f32x4 sc[kStages];
 #pragma unroll
                 for (int st = 0; st < kStages; ++st) sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -137,7 +179,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int n = 0; n < QL; ++n) {
-                        const bf16x8 q = *(const bf16x8*)(q_s[n] + (16 * g + l16) * 256 + (((4 * group + j) ^ l16) * 16));
+                        const bf16x8 q = staged_operand<kChunk>(q_s, n, 16 * g, l16, group, j);
 #pragma unroll
                         for (int st = 0; st < kStages; ++st) sc[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k[st][j], sc[st], 0, 0, 0);
                     }
@@ -166,6 +208,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 const float sum = rows_sum(acc[st]);
                 if (group == st) got = sum;
             }
+            if (SHARED) {
+                float (&sums)[4][kWaveTokens] = sum_s[(v / place.n) & 1];
+                if (lane < kWaveTokens) sums[wave][lane] = got;
+                lds_only_barrier();                              // (the next tile's sums are the other ones)
+                if (wave > 0) return;
+                got = lane < kWaveTokens ? (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]) : 0.f;
+            }
             if (mine) *w_out = r0 > 0 ? before + got : a.w_in ? fmaf(a.decay, before, got) : got;
         };
         for (int v = place.split; v < tiles; v += 2 * place.n) {
@@ -175,12 +224,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     }
 }
 
-template <int P, bool N16>
-void launch(const Args& a, int dt, hipStream_t s) {
+template <int P, bool N16, int QL>
+void launch(const Args& a, bool shared, hipStream_t s) {
     const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)a.H_kv);
-    if (dt == KVBFP_F32) accumulate_weights<P, N16, 3><<<grid, kThreads, 0, s>>>(a);
-    else if (dt == KVBFP_F16) accumulate_weights<P, N16, 2><<<grid, kThreads, 0, s>>>(a);
-    else accumulate_weights<P, N16, 1><<<grid, kThreads, 0, s>>>(a);
+    if (shared) accumulate_weights<P, N16, QL, true><<<grid, kThreads, 0, s>>>(a);
+    else accumulate_weights<P, N16, QL, false><<<grid, kThreads, 0, s>>>(a);
+}
+template <int P, bool N16>
+void launch(const Args& a, int dt, bool shared, hipStream_t s) {
+    if (dt == KVBFP_F32) launch<P, N16, 3>(a, shared, s);
+    else if (dt == KVBFP_F16) launch<P, N16, 2>(a, shared, s);
+    else launch<P, N16, 1>(a, shared, s);
 }
 
 }  // namespace
@@ -203,18 +257,23 @@ static int weights_impl(const char* call, const kvbfp_layout* L, const kvbfp_cac
     if (a.H_kv > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     a.perm_k = perm_k;
     a.lse_in = lse; a.w_in = weights_in; a.w_out = weights_out; a.w_stride = weights_stride; a.decay = decay;
-    // three workgroups per compute unit
-    const int64_t tiles = (max_len + kTileTokens - 1) / kTileTokens, units = (int64_t)a.batch * a.H_kv;
-    a.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, (768 + units - 1) / units));
-    a.share = seq_len_dev && a.batch > 1 && a.batch <= 64 && a.n_splits > 1;
+    // as many workgroups as the compute units have room for: three each, two with fp16 I/O
+    const int64_t units = (int64_t)a.batch * a.H_kv;
+    int64_t tiles = (max_len + 4 * kWaveTokens - 1) / (4 * kWaveTokens);
+    const int64_t round = dtype == KVBFP_F16 ? 512 : 768;
+    const bool shared = a.M > 16 && tiles * units < round;
+    if (shared) tiles = (max_len + kWaveTokens - 1) / kWaveTokens;
+    const bool shares = seq_len_dev && a.batch > 1 && a.batch <= 64;
+    a.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, round_of(round, units, shares)));
+    a.share = shares && a.n_splits > 1;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool n16 = logical.block == 16;
     if (logical.mant_bits == 4) {
-        if (n16) launch<4, true>(a, (int)dtype, s);
-        else launch<4, false>(a, (int)dtype, s);
+        if (n16) launch<4, true>(a, (int)dtype, shared, s);
+        else launch<4, false>(a, (int)dtype, shared, s);
     } else {
-        if (n16) launch<8, true>(a, (int)dtype, s);
-        else launch<8, false>(a, (int)dtype, s);
+        if (n16) launch<8, true>(a, (int)dtype, shared, s);
+        else launch<8, false>(a, (int)dtype, shared, s);
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(KVBFP_ERR_HIP, "%s: %s", call, hipGetErrorString(err));
