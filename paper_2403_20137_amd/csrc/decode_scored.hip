@@ -154,6 +154,20 @@ __device__ __forceinline__ void store_out(const Args& a, int64_t at, float v) {
     typedef typename Io<QL>::T T;
     ((T*)a.out)[at] = (T)v;
 }
+template <int QL>
+__device__ __forceinline__ void store_eight(const Args& a, int64_t at, const float (&v)[8]) {
+    typedef typename Io<QL>::T T;
+    typedef T Tx8 __attribute__((ext_vector_type(8)));
+    Tx8 x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (T)v[i];
+    if (((uintptr_t)a.out & 15u) == 0) {
+        *(Tx8*)((T*)a.out + at) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ((T*)a.out)[at + i] = x[i];
+    }
+}
 __device__ __forceinline__ float natural_lse(float m, float l) {
     return l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
@@ -188,9 +202,17 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
         ml_s[wave][l16][0] = x.ref;
         ml_s[wave][l16][1] = sum;
     }
-    __syncthreads();
     const int row = tid >> 4, p0 = (tid & 15) * 8;
+    int channel[8];
+    if (a.n_splits == 1) {
 #pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            channel[i] = position_channel<P>(p0 + i);
+            if (a.perm_v) channel[i] = a.perm_v[kvh * kD + channel[i]] & (kD - 1);
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
     for (int rw = 0; rw < RW; ++rw) {
         const int r = r0 + 16 * rw + row;
         if (row >= RP || r >= a.M) continue;
@@ -218,14 +240,18 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
             *(f32x4*)(a.part_o + at * kD + p0) = f32x4{acc[0], acc[1], acc[2], acc[3]};
             *(f32x4*)(a.part_o + at * kD + p0 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
         } else {
+            // into the order of the output in LDS, where the row came from (nobody but these 16 lanes looks at it): stores of single
+            // channels took longer than everything before them with 108 rows of two tokens, 23 us against 18.7
             const int64_t at = out_row(a, b, kvh, r);
             const float by = den > 0.f ? up / den : 0.f;
+            float* const row_s = (float*)(smem + rw * kWaveLds) + row * kOStride;
+            wave_fence();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                int ch = position_channel<P>(p0 + i);
-                if (a.perm_v) ch = a.perm_v[kvh * kD + ch] & (kD - 1);
-                store_out<QL>(a, at * kD + ch, acc[i] * by);
-            }
+            for (int i = 0; i < 8; ++i) row_s[channel[i]] = acc[i] * by;
+            wave_fence();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = row_s[p0 + i];
+            store_eight<QL>(a, at * kD + p0, acc);
             if (p0 == 0 && a.lse) a.lse[at] = natural_lse(top, den);
         }
     }
@@ -381,12 +407,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (tid < 2) large_s[tid] = 0;
     for (int i = tid; i < 16 * RW * HC; i += kThreads) rule_s[i] = row_rule(a, s, b, kvh, r0 + i);
     bf16x8 q[HC][QL][4];
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
-        if (c > 0) lds_only_barrier();
-        rows[c].put(a, r0 + 16 * RW * c, (float*)smem, perm_s);
+#pragma unroll 1
+    for (int c = 0;; ++c) {
+        rows[0].put(a, r0 + 16 * RW * c, (float*)smem, perm_s);
         lds_only_barrier();                                  // (the first rows are on their way)
-        query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[c]);
+        query_operand<P, QL>((const float*)smem, perm_s, 16 * rw + l16, group, q[HC - 1]);
+        if (c == HC - 1) break;
+#pragma unroll
+        for (int i = 0; i < QL; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[0][i][j] = q[HC - 1][i][j];
+        rows[0] = rows[HC - 1];
+        lds_only_barrier();
     }
     lds_only_barrier();                                      // the queries give way to keys and values
 
@@ -462,15 +494,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             else add_values<PL, HC>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
         }
     }
-#pragma unroll
-    for (int c = 0; c < HC; ++c) {
+#pragma unroll 1
+    for (int c = 0;; ++c) {                                  // (a loop: code that runs once is as long as its way from memory)
         const int rc = r0 + 16 * RW * c;
         if (RW == 4 && a.n_splits > 1) {                     // nothing to join
-            store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[c], x[c]);
+            store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[0], x[0]);
         } else {
             __syncthreads();
-            if (rc < a.M) finish<P, QL, RW, 16>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[c], x[c]);
+            finish<P, QL, RW, 16>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
         }
+        if (c == HC - 1 || rc + 16 * RW >= a.M) break;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) o[0][ct] = o[HC - 1][ct];
+        x[0] = x[HC - 1];
     }
 }
 
@@ -561,8 +597,14 @@ __global__ __launch_bounds__(kThreads) void scored_combine(Args a) {
     }
 }
 
-// Rows of a workgroup: 16 in scored_split (rw = 1), 16 * rw * hc in scored_split_wide; splits: as many as make one resident round of
-// workgroups (three a compute unit in scored_split, two in scored_split_wide), and no more than there are tiles.
+// Rows of a workgroup: 16 in scored_split (rw = 1), 16 * rw * hc in scored_split_wide.  More of them decode a tile for more rows, fewer take less
+// time for a tile: 64 rows instead of 32 from kFourFrom tiles on (8 x 64 rows of 300 and 1000 tokens 11.8 and 12.1 us with 64 rows, 10.4 and 11.3
+// with 32; 48 x 60 rows of 3000 30.2 and 31.6), 128 (with bf16 I/O, which has the registers for it) from kTwoFrom on (32 x 256 rows of 3000
+// and 24000 tokens 52.7 and 212 us with 128 rows, 44.4 and 219 with 64).
+// Splits: as many as make one resident round of workgroups (three a compute unit in scored_split, two in scored_split_wide) and no more
+// than there are tiles; none where the partial results and the second kernel would take longer than a few more tiles (32 x 256
+// rows of 200 and 400 tokens 19.3 and 21.9 us in two splits, 13.0 and 16.7 in one; 8 x 4 rows of 400 8.6 in four, 10.6 in one).
+constexpr int64_t kFourFrom = 1024, kTwoFrom = 8192;
 struct Plan { int32_t hc, rw, row_tiles, n_splits; };
 
 template <int P, bool N16, int QL>
@@ -601,25 +643,24 @@ void launch_combine(const Args& a, int dt, hipStream_t s) {
     else launch_combine<P, 1>(a, s);
 }
 
-// The most splits that a call takes; the workspace, which does not depend on the type, has room for them.
-int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len, bool shares) {
-    const int64_t of_wg = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads * ((rows + of_wg - 1) / of_wg);
-    const int64_t tile = rows > 16 ? kWideTokens : kTileTokens, tiles = (max_len + tile - 1) / tile;
-    const int64_t wanted = rows <= 16 ? 768 : 512;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, round_of(wanted, units, shares)));
-}
 Plan plan(const kvbfp_layout* L, int64_t rows, int64_t max_len, int dtype, bool shares) {
+    const int64_t units = (int64_t)L->batch * L->n_kv_heads, tiles = (max_len + kWideTokens - 1) / kWideTokens;
+    const auto parts = [&](int64_t of_wg) { return units * ((rows + of_wg - 1) / of_wg); };
     Plan p;
-    p.hc = rows > 64 && dtype == KVBFP_BF16 ? 2 : 1;
-    p.rw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t of_wg = 16 * p.hc * p.rw;
+    p.rw = rows <= 16 ? 1 : rows <= 32 || parts(64) * tiles < kFourFrom ? 2 : 4;
+    p.hc = rows > 64 && dtype == KVBFP_BF16 && parts(128) * tiles >= kTwoFrom ? 2 : 1;
+    const int64_t of_wg = 16 * p.hc * p.rw, steps = p.rw == 1 ? (max_len + kTileTokens - 1) / kTileTokens : tiles;
     p.row_tiles = (int32_t)((rows + of_wg - 1) / of_wg);
-    // (fp16 and fp32 have more, smaller workgroups: one resident round all the same)
-    const int64_t units = (int64_t)L->batch * L->n_kv_heads * p.row_tiles;
-    p.n_splits = splits_of(L, rows, max_len, shares);
-    if (p.rw > 1) p.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(p.n_splits, round_of(512, units, shares)));
+    const bool one = steps <= 2 + std::min<int64_t>(units * rows / 1024, 8);
+    p.n_splits = one ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>(steps, round_of(p.rw == 1 ? 768 : 512, parts(of_wg), shares)));
     return p;
+}
+// The most splits that a call takes, whatever its type and lengths: the workspace has room for them.
+int32_t splits_of(const kvbfp_layout* L, int64_t rows, int64_t max_len) {
+    int32_t most = 1;
+    for (int dtype : {KVBFP_BF16, KVBFP_F16})
+        for (bool shares : {false, true}) most = std::max(most, plan(L, rows, max_len, dtype, shares).n_splits);
+    return most;
 }
 
 size_t partial_bytes(const kvbfp_layout* L, int64_t rows, int32_t n_splits) {
@@ -741,7 +782,7 @@ size_t kvbfp_scored_workspace_bytes(const kvbfp_layout* L, int32_t n_q_heads, in
         return 0;
     }
     const int64_t rows = (int64_t)(n_q_heads / L->n_kv_heads) * n_q_tokens;
-    return std::max<size_t>(partial_bytes(L, rows, splits_of(L, rows, max_len, true)), 256);
+    return std::max<size_t>(partial_bytes(L, rows, splits_of(L, rows, max_len)), 256);
 }
 
 size_t kvbfp_scored_workspace_bytes_paged(const kvbfp_layout* pool, int64_t table_stride, int32_t batch, int32_t n_q_heads,
