@@ -437,10 +437,11 @@ int kvbfp_decode_attention_noalloc(const kvbfp_layout* layout, const kvbfp_cache
  * and sees it if t < seq_len and
  *     t < prefix_dev[b]   or   ( order(i, t)  and  t >= first_dev[b][i]  and  (window == 0 or pos(i) - pos(t) < window) )
  *   order : t < base, or node t - base is one that i sees: bit t - base of tree_mask[b][i] (bits of i's ancestors and of i itself in a tree
- *           of drafted tokens; any mask will do, a node that sees nothing is fine), without tree_mask the nodes up to i itself.
+ *           of drafted tokens; any mask will do, a node that sees nothing is fine, bits from n_q_tokens on mean nothing), without
+ *           tree_mask the nodes up to i itself.
  *   pos   : t for t < base; for node j base + the number of other nodes that it sees (its depth in the tree; base + j without one).
  * A query token that sees nothing yields zeros and lse = -infinity.
- *   cap        : finite, >= 0; 0 = none.
+ *   cap        : finite, >= 0; 0 = none.  Refused where softmax_scale / cap passes fp32's range.
  *   window     : >= 0; 0 = none.
  *   slopes     : DEVICE float [n_q_heads] or NULL.
  *   first_dev  : DEVICE int32 [batch][n_q_tokens] or NULL: the first token of the document that a query token belongs to.
@@ -492,7 +493,7 @@ int kvbfp_decode_attention_scored_paged(const kvbfp_layout* pool, const kvbfp_ca
  * lengths (a row whose lse is -infinity adds nothing).  Reads the keys alone, once.
  *   lse         : DEVICE float [batch][n_q_tokens][n_q_heads].
  *   weights_in  : DEVICE float [batch][n_kv_heads][weights_stride], or NULL = zeros (decay is then not looked at).
- *   weights_out : DEVICE, the same shape; may be weights_in itself.  Tokens from seq_len on are left as they are.
+ *   weights_out : DEVICE, the same shape; may be weights_in itself (but not overlap it otherwise).  Tokens from seq_len on are left as they are.
  *   cache       : the value planes may be NULL.
  * No atomics: the same bits every time.  Errors: INVALID_ARG (also weights_stride < max_len), UNSUPPORTED, HIP. */
 int kvbfp_accumulate_weights(const kvbfp_layout* layout, const kvbfp_cache* cache, int32_t n_q_heads, int32_t n_q_tokens,

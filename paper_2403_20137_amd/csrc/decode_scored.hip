@@ -712,6 +712,8 @@ int fill_args(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache,
     while ((1 << a->log2_block) < logical->block) ++a->log2_block;
     constexpr float kLog2e = 1.4426950408889634f;
     a->score_mul = softmax_scale * kLog2e;
+    if (!std::isfinite(a->score_mul * 128.f))                // (times the scale of the decoded codes)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: softmax_scale = %g", call, (double)softmax_scale);
     if (paging) {
         a->block_table = paging->block_table; a->table_stride = paging->table_stride; a->n_pages = L->batch;
         while (((int64_t)1 << a->log2_page) < L->max_seq) ++a->log2_page;
@@ -720,7 +722,9 @@ int fill_args(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache,
         if (rule->cap > 0.f) {
             a->cap = rule->cap * kLog2e;
             a->inv_cap = 1.f / a->cap;
-            if (!std::isfinite(a->cap) || !std::isfinite(a->inv_cap)) return fail(KVBFP_ERR_INVALID_ARG, "%s: rule.cap = %g", call, (double)rule->cap);
+            // (what scores are multiplied with on their way into the exponential, with the scale of the decoded codes)
+            const float turn = a->inv_cap * 2.8853900817779268f * std::max(1.f, std::fabs(a->score_mul) * 128.f);
+            if (!std::isfinite(a->cap) || !std::isfinite(turn)) return fail(KVBFP_ERR_INVALID_ARG, "%s: rule.cap = %g", call, (double)rule->cap);
         }
         a->slopes = rule->slopes; a->first = rule->first_dev; a->prefix = rule->prefix_dev;
         a->tree = rule->tree_mask; a->tree_stride = rule->tree_stride;

@@ -126,9 +126,9 @@ __device__ __forceinline__ Place places_of(const Args& a, int b) {
     return p;
 }
 
-// Nodes that node i of sequence b sees.
+// Nodes that node i of sequence b sees (bits behind the last node mean nothing).
 __device__ __forceinline__ uint64_t node_mask(const Args& a, int b, int i) {
-    if (a.tree) return a.tree[(int64_t)b * a.tree_stride + i];
+    if (a.tree) return a.tree[(int64_t)b * a.tree_stride + i] & (~0ull >> (64 - a.n_tok));
     return i >= 63 ? ~0ull : (2ull << i) - 1;
 }
 // Its position behind the tokens before the nodes: how many others it sees.

@@ -253,6 +253,10 @@ static int weights_impl(const char* call, const kvbfp_layout* L, const kvbfp_cac
     if (!lse || !weights_out) return fail(KVBFP_ERR_INVALID_ARG, "%s: lse/weights_out is NULL", call);
     if (weights_stride < max_len)
         return fail(KVBFP_ERR_INVALID_ARG, "%s: weights_stride %lld below max_len %lld", call, (long long)weights_stride, (long long)max_len);
+    const size_t bytes = (size_t)a.batch * (size_t)a.H_kv * (size_t)weights_stride * sizeof(float);
+    if (weights_in && weights_in != weights_out && (uintptr_t)weights_in < (uintptr_t)weights_out + bytes &&
+        (uintptr_t)weights_out < (uintptr_t)weights_in + bytes)
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: weights_out overlaps weights_in without being the same", call);
     if (!std::isfinite(decay)) return fail(KVBFP_ERR_INVALID_ARG, "%s: decay is not finite", call);
     if (a.H_kv > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     a.perm_k = perm_k;

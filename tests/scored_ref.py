@@ -35,7 +35,7 @@ def decoded(cache, which, table=None, length=None):
 def seen_and_far(n, size, mask=None, window=0, first=None, prefix=0):
     """bool [n][size], int [n][size] for one sequence of `size` tokens whose last n are the query tokens."""
     base = size - n
-    masks = [(2 << i) - 1 for i in range(n)] if mask is None else [int(x) & (2 ** 64 - 1) for x in mask]
+    masks = [(2 << i) - 1 for i in range(n)] if mask is None else [int(x) & (2 ** n - 1) for x in mask]
     depth = [bin(m & ~(1 << i)).count("1") for i, m in enumerate(masks)]
     seen, far = np.zeros((n, size), bool), np.zeros((n, size), np.int64)
     for i in range(n):

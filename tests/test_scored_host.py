@@ -45,6 +45,7 @@ def test_scored_attention_refusals():
     assert attend(dtype=7) == BAD
     assert attend(max_len=0) == BAD and attend(max_len=513) == BAD
     assert attend(scale=float("nan")) == BAD and attend(scale=float("inf")) == BAD
+    assert attend(scale=3e38) == BAD and attend(scale=-3e38) == BAD
     assert attend(cache=kvbfp.CachePtrs(0x100000, 0x200000, 0, 0)) == BAD
     assert attend(cache=kvbfp.CachePtrs(0x100008, 0x200000, 0x300000, 0x400000)) == BAD
     assert attend(layout=kvbfp.make_layout(64, 32, 4, 2, 3, 512)) == UNS
@@ -58,6 +59,9 @@ def test_rule_refusals():
         assert "rule" in kvbfp.last_error()
     for good in (dict(), dict(cap=50.0), dict(window=2 ** 31 - 1), dict(tree_mask=0x10000, tree_stride=0), dict(tree_mask=0x10000, tree_stride=9)):
         assert attend(r=rule(**good)) == WS, good
+    # the scale over the cap: 2e6 * 128 * 2.9 / 1e-30 is no fp32 number; 0.1 over it is one
+    assert attend(r=rule(cap=1e-30), scale=2e6) == BAD and "cap" in kvbfp.last_error()
+    assert attend(r=rule(cap=1e-30), scale=0.1) == WS and attend(r=rule(cap=1e-38)) == BAD
 
 
 def test_paged_refusals():
@@ -72,15 +76,27 @@ def test_paged_refusals():
     assert kvbfp.scored_workspace_bytes(LAYOUT, 8, 4, 513) == 0 and kvbfp.scored_workspace_bytes_paged(POOL, 0, 3, 8, 4, 512) == 0
 
 
-def collect(layout=LAYOUT, cache=PTRS, heads=8, tokens=4, q=FAKE, max_len=512, lse=FAKE, decay=1.0, out=FAKE, stride=512, r=None, scale=0.1):
+def collect(layout=LAYOUT, cache=PTRS, heads=8, tokens=4, q=FAKE, max_len=512, lse=FAKE, decay=1.0, out=FAKE, stride=512, r=None, scale=0.1,
+            before=None):
     return kvbfp.lib().kvbfp_accumulate_weights(C.byref(layout), C.byref(cache), heads, tokens, q, kvbfp.BF16, None, max_len, scale, None, r,
-                                                lse, decay, None, out, stride, None)
+                                                lse, decay, before, out, stride, None)
 
 
 def test_weights_refusals():
     for bad in (dict(lse=None), dict(out=None), dict(stride=511), dict(decay=float("nan")), dict(heads=3), dict(tokens=65), dict(q=None),
                 dict(max_len=600), dict(cache=kvbfp.CachePtrs(0, 0x200000, 0, 0)), dict(r=rule(cap=-2.0)), dict(scale=float("nan"))):
         assert collect(**bad) == BAD, bad
+    for shift in (4, -4, 3 * 2 * 512 * 4 - 4, 4 - 3 * 2 * 512 * 4):          # neither the same nor apart
+        assert collect(out=C.c_void_p(0x1000000), before=C.c_void_p(0x1000000 + shift)) == BAD and "overlap" in kvbfp.last_error()
+
+
+def test_workspace_grows_with_the_length():
+    # a workspace for the longest call holds shorter ones, whatever way they are split
+    for heads, batch, rows in ((2, 3, 512), (8, 70, 4096), (8, 8, 40000)):
+        layout = kvbfp.make_layout(128, 32, 4, heads, batch, rows)
+        for group, tokens in ((4, 1), (4, 5), (12, 5), (4, 32), (4, 64), (17, 8)):
+            sizes = [kvbfp.scored_workspace_bytes(layout, heads * group, tokens, n) for n in range(1, rows + 1, 61)]
+            assert sizes == sorted(sizes), (heads, batch, group, tokens)
 
 
 def evict(src=LAYOUT, dst=kvbfp.make_layout(128, 32, 4, 2, 3, 100), cache=PTRS, to=OTHER, w=0x5000000, stride=512, lens=None, max_len=512, keep=100,
