@@ -252,35 +252,46 @@ __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const 
     return factor;
 }
 
-// The same for N rows (rule_s[0] ..) of one token t, exactly; everything multiplied.
-template <int N>
-__device__ __forceinline__ void rule_token(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t, float mul, float (&y)[N]) {
+// The same for four rows (rule_s[0] ..) of the ST tokens t0 + 16 st, y[4 st + row], exactly; everything multiplied.
+template <int ST>
+__device__ __forceinline__ void rule_tokens(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t0, float mul,
+                                            float (&y)[4 * ST]) {
     if (a.cap != 0.f) {
-        cap_scores<N, true>(y, mul, a.cap, a.inv_cap);
+#pragma unroll
+        for (int st = 0; st < ST; ++st) {
+            float v[4] = {y[4 * st], y[4 * st + 1], y[4 * st + 2], y[4 * st + 3]};
+            cap_scores<4, true>(v, mul, a.cap, a.inv_cap);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[4 * st + i] = v[i];
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) y[i] *= mul;
+        for (int i = 0; i < 4 * ST; ++i) y[i] *= mul;
     }
     if (inner) {
         if (a.slopes) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = fmaf(-rule_s[i].slope, (float)(rule_s[i].pos - t), y[i]);
+            for (int i = 0; i < 4 * ST; ++i) y[i] = fmaf(-rule_s[i & 3].slope, (float)(rule_s[i & 3].pos - (t0 + 16 * (i >> 2))), y[i]);
         }
         return;
     }
-    const int node = t - s.base;
+    int depth[ST];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int st = 0; st < ST; ++st) depth[st] = depth_s[(t0 + 16 * st - s.base) & 63];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
         const RowRule u = rule_s[i];
-        bool seen = t >= u.lo;
-        int far = u.pos - t;
-        if (node >= 0) {
-            far = u.pos - s.base - depth_s[node & 63];
-            seen = ((u.nodes >> (node & 63)) & 1) && t >= u.first && (a.window == 0 || far < a.window);
+#pragma unroll
+        for (int st = 0; st < ST; ++st) {                    // (both answers, one taken: a branch would wait for each read by itself)
+            const int t = t0 + 16 * st, node = t - s.base;
+            const bool drafted = node >= 0;
+            const int far = u.pos - (drafted ? s.base + depth[st] : t);
+            const bool near = (((u.nodes >> (node & 63)) & 1) != 0) & (t >= u.first) & ((a.window == 0) | (far < a.window));
+            const bool seen = ((drafted ? near : t >= u.lo) | (t < s.prefix)) & (t < s.len);
+            float v = y[4 * st + i];
+            if (a.slopes) v = fmaf(-u.slope, fabsf((float)far), v);
+            y[4 * st + i] = seen ? v : -INFINITY;
         }
-        seen = (seen || t < s.prefix) && t < s.len;
-        if (a.slopes) y[i] = fmaf(-u.slope, fabsf((float)far), y[i]);
-        y[i] = seen ? y[i] : -INFINITY;
     }
 }
 

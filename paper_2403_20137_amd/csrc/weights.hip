@@ -77,6 +77,7 @@ struct StagedRows {
 #pragma unroll
         for (int p = 0; p < EARLY; ++p)
             if (p == 0 || r0 + 16 * p < a.M) put16(p, first[p]);
+#pragma unroll 1
         for (int p = EARLY; p < ROWS / 16 && r0 + 16 * p < a.M; ++p) put16(p, load(a, b, kvh, r0 + 16 * p));
     }
 };
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         struct Tile {
             Chunk<P, N16> raw[kStages];
             float before;                                        // what the lane's token has so far
-        } next[2];                                               // two tiles in flight
+        } next;                                                  // one tile in flight
         auto sees = [&](int t0) { return t0 < s.len && (t0 < s.prefix || t0 + kWaveTokens > min(lo_least, max(s.base, 0))); };
         // (without a branch: a load whose result meets another value behind it would be waited for there.  Tiles behind the last one and
         // those that no row sees stand for something that is read anyway.)
@@ -137,8 +138,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
                 load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), at, to.raw[st]);
             }
         };
-        request(place.split, next[0]);
-        request(place.split + place.n, next[1]);
+        request(place.split, next);
         queries.place(at_s);
         lds_only_barrier();                                      // at_s is complete; nobody looks at the rows before these any more
         const int rows = min(a.M - r0, kChunk), groups = (rows + 15) / 16;
@@ -170,9 +170,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 #pragma unroll
                     for (int j = 0; j < 4; ++j) k[st][j] = __builtin_bit_cast(bf16x8, eight<P, N16>(from.raw[st], j));
             }
-            request(v + 2 * place.n, from);
-            for (int g = SHARED ? wave : 0; seen && g < groups; g += kStep) {
-                f32x4 sc[kStages];
+            request(v + place.n, from);
+            auto scores = [&](int g, f32x4 (&sc)[kStages]) {
 #pragma unroll
                 for (int st = 0; st < kStages; ++st) sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -183,22 +182,30 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 #pragma unroll
                         for (int st = 0; st < kStages; ++st) sc[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k[st][j], sc[st], 0, 0, 0);
                     }
-                const f32x4 ref = *(const f32x4*)(ref_s + 16 * g + 4 * group);
-                if (a.cap == 0.f && !a.slopes && inner) {
+            };
+            if (seen && inner && a.cap == 0.f && !a.slopes) {
+#pragma unroll 1
+                for (int g = SHARED ? wave : 0; g < groups; g += kStep) {
+                    f32x4 sc[kStages];
+                    scores(g, sc);
+                    const f32x4 ref = *(const f32x4*)(ref_s + 16 * g + 4 * group);
 #pragma unroll
                     for (int st = 0; st < kStages; ++st)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[st] += exp2_raw(fmaf(sc[st][i], mul, ref[i]));
-                } else {
+                }
+            } else if (seen) {
+#pragma unroll 1
+                for (int g = SHARED ? wave : 0; g < groups; g += kStep) {
+                    f32x4 sc[kStages];
+                    scores(g, sc);
+                    const f32x4 ref = *(const f32x4*)(ref_s + 16 * g + 4 * group);
+                    float y[4 * kStages];
 #pragma unroll
-                    for (int st = 0; st < kStages; ++st) {
-                        float y[4];
+                    for (int i = 0; i < 4 * kStages; ++i) y[i] = sc[i >> 2][i & 3];
+                    rule_tokens<kStages>(a, s, rule_s + 16 * g + 4 * group, depth_s, inner, t0 + l16, mul, y);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = sc[st][i];
-                        rule_token<4>(a, s, rule_s + 16 * g + 4 * group, depth_s, inner, t0 + 16 * st + l16, mul, y);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[st] += exp2_raw(y[i] + ref[i]);
-                    }
+                    for (int i = 0; i < 4 * kStages; ++i) acc[i >> 2] += exp2_raw(y[i] + ref[i & 3]);
                 }
             }
             // lane: token 16 group + l16
@@ -217,10 +224,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             }
             if (mine) *w_out = r0 > 0 ? before + got : a.w_in ? fmaf(a.decay, before, got) : got;
         };
-        for (int v = place.split; v < tiles; v += 2 * place.n) {
-            step(v, next[0]);
-            step(v + place.n, next[1]);
-        }
+        for (int v = place.split; v < tiles; v += place.n) step(v, next);
     }
 }
 
