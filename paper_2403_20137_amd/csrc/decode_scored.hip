@@ -10,6 +10,15 @@
 // The query is not rounded (bf16 one operand, fp16 two, fp32 three); probabilities are two bf16 limbs (16 bits), three with fp32 I/O.
 // A tile of 32 tokens whose tokens all precede the drafted ones and are seen by every row takes no mask; tiles that no row
 // sees (outside the window, the documents and the prefix) are not read.
+//
+// What bounds it.  Few rows and long sequences: 8 x 8 heads of 32768 tokens, four rows each, capped scores, 64 us (4.4 TB/s; the same
+// without the cap 61; 45 at the rate of a reading kernel): decoding to bf16 and the softmax take vector instructions about as long as the reading,
+// and three workgroups a compute unit overlap the two only in part.  Many rows: matrix and vector instructions, which hardly overlap within
+// a compute unit: 8 sequences of 8192 tokens with trees of 64 (256 rows a kv-head) 150 us, 300 TFLOP/s of the two products; the second limb of the
+// probabilities is a third of the matrix work and stays, as one bf16 is off by 2^-9 of every weight.  A short sequence: the way of
+// the first loads and of the code itself, 7 to 9 us; loops that run once are not unrolled where that only makes them longer.
+// Measured and not kept: products of the next tile ahead of the values of this one, two tiles in flight, four workgroups a compute unit, 32 rows a
+// wavefront for 33 to 64 rows, rows of the output stored by channels.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -187,8 +196,8 @@ __device__ __forceinline__ void store_partial(const Args& a, int kvh, int r0, in
     if (group == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(x.ref, sum);
 }
 // The sums of a workgroup's wavefronts for RP * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
-// 16 (w % RW) .., or twice the same 8 rows, RP = 8, RW = 1) and written as this split's partial result, or as the output where there is one split.  smem: four times kWaveLds,
-// free when this is called.
+// 16 (w % RW) .., or twice the same 8 rows, RP = 8, RW = 1) and written as this split's partial result, or as the output
+// where there is one split.  smem: four times kWaveLds, free when this is called.
 template <int P, int QL, int RW, int RP>
 __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int place, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
                                        const f32x4 (&o)[8], const Running& x) {
@@ -259,7 +268,7 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
 
 // Up to 16 rows: every wavefront has all of them and takes 32 tokens of a tile of 128 for itself.  With up to 8 rows (RP = 8) the 16
 // columns are these rows twice, once for either stage of 16 tokens: each lane then has four scores instead of eight, half of which would
-// be nobody's; the columns are joined in the end like another wavefront's.
+// be nobody's; the columns are joined in the end like another wavefront's (8 x 32768 tokens 68 us with them once, 64.5 twice).
 // grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL bf16 numbers of a query.
 template <int P, bool N16, int QL, int RP>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
@@ -628,7 +637,9 @@ void launch_split(const Args& a, int dt, const Plan& p, hipStream_t s) {
     else launch_split<P, false, 1>(a, p, s);
 }
 
-// Few rows: four wavefronts for each.
+// Few rows: four wavefronts for each, which share its splits (32 rows in 6 splits and an fp32 tree of 22 rows a kv-head: 8.7 and 11.6 us, with one
+// for four rows 10.9 and 19.9); many: one for four rows, the same work with fewer wavefronts (16384 rows in four splits 150.3 us in all, with
+// four for each 152).
 template <int P, int QL>
 void launch_combine(const Args& a, hipStream_t s) {
     const int64_t rows = (int64_t)a.batch * a.H_kv * a.M;
