@@ -12,9 +12,9 @@
 // sees (outside the window, the documents and the prefix) are not read.
 //
 // What bounds it.  Few rows and long sequences: 8 x 8 heads of 32768 tokens, four rows each, capped scores, 64 us (4.4 TB/s; the same
-// without the cap 61; 45 at the rate of a reading kernel): decoding to bf16 and the softmax take vector instructions about as long as the reading,
+// without the cap 62; 45 at the rate of a reading kernel): decoding to bf16 and the softmax take vector instructions about as long as the reading,
 // and three workgroups a compute unit overlap the two only in part.  Many rows: matrix and vector instructions, which hardly overlap within
-// a compute unit: 8 sequences of 8192 tokens with trees of 64 (256 rows a kv-head) 150 us, 300 TFLOP/s of the two products; the second limb of the
+// a compute unit: 8 sequences of up to 8192 tokens with trees of 64 (256 rows a kv-head, capped) 150 us, 300 TFLOP/s of the two products; the second limb of the
 // probabilities is a third of the matrix work and stays, as one bf16 is off by 2^-9 of every weight.  A short sequence: the way of
 // the first loads and of the code itself, 7 to 9 us; loops that run once are not unrolled where that only makes them longer.
 // Measured and not kept: products of the next tile ahead of the values of this one, two tiles in flight, four workgroups a compute unit, 32 rows a
