@@ -647,7 +647,7 @@ def _check_rule(rule, batch, n_tok, n_q_heads):
     slopes, first, prefix, tree = rule.tensors
     if slopes is not None and slopes.shape[0] != n_q_heads:
         raise ValueError("slopes must be [n_q_heads]")
-    if first is not None and tuple(first.shape) != (batch, n_tok):
+    if first is not None and first.shape != (batch, n_tok):
         raise ValueError("first_dev must be [batch][n_q_tokens]")
     if prefix is not None and prefix.shape[0] != batch:
         raise ValueError("prefix_dev must be [batch]")
@@ -657,12 +657,14 @@ def _check_rule(rule, batch, n_tok, n_q_heads):
 
 
 def _check_queries(q, batch, head_dim):
-    if q.dim() != 4 or not q.is_contiguous() or q.shape[0] != batch or q.shape[3] != head_dim or q.dtype not in _TORCH_DT:
+    shape = q.shape
+    if len(shape) != 4 or not q.is_contiguous() or shape[0] != batch or shape[3] != head_dim or q.dtype not in _TORCH_DT:
         raise ValueError("q must be a contiguous [batch][n_q_tokens][n_q_heads][head_dim] tensor")
+    return shape
 
 
 def _check_float(t, what, shape):
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor %s" % (what, list(shape)))
 
 
@@ -672,7 +674,7 @@ def _check_like_q(out, q):
 
 
 def _check_lens(seq_len_dev, batch):
-    if seq_len_dev is not None and (tuple(seq_len_dev.shape) != (batch,) or not seq_len_dev.is_contiguous()):
+    if seq_len_dev is not None and (seq_len_dev.shape != (batch,) or not seq_len_dev.is_contiguous()):
         raise ValueError("seq_len_dev must be a contiguous int32 tensor [batch]")
 
 
@@ -687,8 +689,8 @@ def scored_workspace_bytes_paged(pool_layout: Layout, pages_per_seq, batch, n_q_
 
 def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_dev, perm_k, perm_v, out, lse, workspace, stream):
     L = cache.layout
-    _check_queries(q, batch, L.head_dim)
-    n_tok, n_q_heads = q.shape[1], q.shape[2]
+    shape = _check_queries(q, batch, L.head_dim)
+    n_tok, n_q_heads = shape[1], shape[2]
     rule = _check_rule(rule, batch, n_tok, n_q_heads)
     _check_lens(seq_len_dev, batch)
     if out is None:
@@ -696,7 +698,7 @@ def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_
     else:
         _check_like_q(out, q)
     if lse is not None:
-        _check_float(lse, "lse", q.shape[:3])
+        _check_float(lse, "lse", shape[:3])
     if workspace is None:
         need = scored_workspace_bytes(L, n_q_heads, n_tok, max_len) if block_table is None else \
             scored_workspace_bytes_paged(L, block_table.shape[1], batch, n_q_heads, n_tok, max_len)
@@ -706,7 +708,7 @@ def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_
     ptrs = cache.ptrs
     rest = (n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
             _dev_ptr(perm_k, torch.int32), _dev_ptr(perm_v, torch.int32), rule, _dev_ptr(out), _dev_ptr(lse), _dev_ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+            workspace.nbytes, _stream_ptr(stream))
     if block_table is None:
         _check(lib().kvbfp_decode_attention_scored(C.byref(L), C.byref(ptrs), *rest))
     else:
@@ -730,22 +732,23 @@ def decode_attention_scored_paged(pool: Cache, block_table, q, max_len, softmax_
 
 def _accumulate(cache, block_table, batch, q, max_len, softmax_scale, lse, weights_in, weights_out, decay, rule, seq_len_dev, perm_k, stream):
     L = cache.layout
-    _check_queries(q, batch, L.head_dim)
-    n_tok, n_q_heads = q.shape[1], q.shape[2]
+    shape = _check_queries(q, batch, L.head_dim)
+    n_tok, n_q_heads = shape[1], shape[2]
     rule = _check_rule(rule, batch, n_tok, n_q_heads)
     _check_lens(seq_len_dev, batch)
-    _check_float(lse, "lse", q.shape[:3])
+    _check_float(lse, "lse", shape[:3])
     if weights_out is None:
         weights_out = torch.zeros((batch, L.n_kv_heads, max_len), dtype=torch.float32, device=q.device) if weights_in is None else weights_in
-    if weights_out.dim() != 3:
+    size = weights_out.shape
+    if len(size) != 3:
         raise ValueError("weights_out must be [batch][n_kv_heads][tokens]")
-    _check_float(weights_out, "weights_out", (batch, L.n_kv_heads, weights_out.shape[2]))
-    if weights_in is not None:
-        _check_float(weights_in, "weights_in", weights_out.shape)
+    _check_float(weights_out, "weights_out", (batch, L.n_kv_heads, size[2]))
+    if weights_in is not None and weights_in is not weights_out:
+        _check_float(weights_in, "weights_in", size)
     ptrs = cache.ptrs
     rest = (n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
             _dev_ptr(perm_k, torch.int32), rule, _dev_ptr(lse), float(decay), _dev_ptr(weights_in), _dev_ptr(weights_out),
-            weights_out.shape[2], _stream_ptr(stream))
+            size[2], _stream_ptr(stream))
     if block_table is None:
         _check(lib().kvbfp_accumulate_weights(C.byref(L), C.byref(ptrs), *rest))
     else:
@@ -769,17 +772,18 @@ def accumulate_weights_paged(pool: Cache, block_table, q, max_len, softmax_scale
 
 
 def _evict_args(batch, heads, weights, max_len, n_keep, n_first, n_recent, kept, new_len, weights_out, seq_len_dev, stream):
-    if weights.dim() != 3:
+    size = weights.shape
+    if len(size) != 3:
         raise ValueError("weights must be [batch][n_kv_heads][tokens]")
-    _check_float(weights, "weights", (batch, heads, weights.shape[2]))
-    if tuple(kept.shape) != (batch, heads, n_keep) or not kept.is_contiguous():
+    _check_float(weights, "weights", (batch, heads, size[2]))
+    if kept.shape != (batch, heads, n_keep) or not kept.is_contiguous():
         raise ValueError("kept must be a contiguous int32 tensor [batch][n_kv_heads][n_keep]")
-    if tuple(new_len.shape) != (batch,) or not new_len.is_contiguous():
+    if new_len.shape != (batch,) or not new_len.is_contiguous():
         raise ValueError("new_len must be a contiguous int32 tensor [batch]")
     if weights_out is not None:
         _check_float(weights_out, "weights_out", (batch, heads, n_keep))
     _check_lens(seq_len_dev, batch)
-    return (_dev_ptr(weights), weights.shape[2], _dev_ptr(seq_len_dev, torch.int32), int(max_len), int(n_keep), int(n_first), int(n_recent),
+    return (_dev_ptr(weights), size[2], _dev_ptr(seq_len_dev, torch.int32), int(max_len), int(n_keep), int(n_first), int(n_recent),
             _dev_ptr(kept, torch.int32), _dev_ptr(new_len, torch.int32), _dev_ptr(weights_out), _stream_ptr(stream))
 
 
