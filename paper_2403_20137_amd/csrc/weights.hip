@@ -5,10 +5,9 @@
 // groups are added once at the end: no atomics, the same bits every time.  A wavefront has 32 tokens at a time as operands (the keys go
 // from memory to the operand, 32 channels a lane) and goes through up to 128 rows (fp32 I/O 64), which lie in LDS as operands; more rows are
 // further passes over the keys, which add to what the pass before has written.
-// 8 x 8 heads of 32768 tokens, four rows each: 43 us, 3.7 TB/s; 217 vector instructions for 32 tokens (72 of them decode) are 25 us on all compute
-// units, the reading alone would be 25.  Many rows are bound by the exponentials, few tokens by the way of the code and of the first
-// loads: one tile in flight with the loop once took 22.5 us for 4 x 265 rows of 78 tokens where two with the loop twice took 26.9, and as long for
-// long sequences.
+// 8 x 8 heads of 32768 tokens, four rows each: 35 us, 4.5 TB/s (25 for the reading alone, vector instructions 14).  Many rows are bound by the
+// exponentials, few tokens by the way of the code and of the first loads: one tile in flight with the loop once took 22.5 us for 4 x 265 rows of 78
+// tokens where two with the loop twice took 26.9, and as long for long sequences.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -91,6 +90,22 @@ __device__ __forceinline__ bf16x8 staged_operand(const uint8_t* q_s, int n, int 
     return *(const bf16x8*)(q_s + n * (ROWS * 256) + (r0 + l16) * 256 + (((4 * group + j) ^ l16) * 16));
 }
 
+// -lse of a row in base 2; minus infinity: the row has no weights to give.
+__device__ __forceinline__ float reference(const Args& a, int b, int kvh, int r) {
+    if (r >= a.M) return -INFINITY;
+    const int tok = r / a.G;
+    const float lse = a.lse_in[((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)];
+    return lse != -INFINITY ? -lse * 1.4426950408889634f : -INFINITY;
+}
+// v[i] summed over the four groups of 16 lanes, for group i: two exchanges of halves, one of quarters.
+__device__ __forceinline__ float groups_sum(const float (&v)[4]) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[0]), __float_as_uint(v[2]), false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[1]), __float_as_uint(v[3]), false, false);
+    const float even = __uint_as_float(x[0]) + __uint_as_float(x[1]), odd = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    const auto z = __builtin_amdgcn_permlane16_swap(__float_as_uint(even), __float_as_uint(odd), false, false);
+    return __uint_as_float(z[0]) + __uint_as_float(z[1]);
+}
+
 // grid = (n_splits * B, H_kv); QL bf16 numbers of a query.  SHARED: the four wavefronts have the same 32 tokens and every fourth 16 rows, and
 // add up in LDS, where there are too few tokens for a resident round of workgroups that have 32 for each wavefront (16 x 128 rows of 3000 tokens:
 // 25.4 us by tokens, 20.5 shared).
@@ -149,15 +164,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
         const int rows = min(a.M - r0, kChunk), groups = (rows + 15) / 16;
         queries.put(a, b, kvh, r0, q_s, at_s);
         if (tid < kChunk) {
-            const int r = r0 + tid;
-            rule_s[tid] = row_rule(a, s, b, kvh, r);
-            float ref = -INFINITY;
-            if (r < a.M) {
-                const int tok = r / a.G;
-                const float lse = a.lse_in[((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G)];
-                if (lse != -INFINITY) ref = -lse * 1.4426950408889634f;
-            }
-            ref_s[tid] = ref;
+            rule_s[tid] = row_rule(a, s, b, kvh, r0 + tid);
+            ref_s[tid] = reference(a, b, kvh, r0 + tid);
         }
         lds_only_barrier();
         auto step = [&](int v, Tile& from) {
@@ -233,17 +241,117 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     }
 }
 
+// Up to 16 rows of long sequences: the queries stay in registers, a wavefront has 64 tokens at a time, whose keys are decoded and multiplied
+// stage by stage, and in the end a token of its own in each lane: 125 vector instructions for 32 tokens instead of 217, and more wavefronts.  From one
+// workgroup a compute unit on: 8 x 8 heads of 32768 tokens 44.8 -> 35 us, ragged 16 x 32 of 1000 20.4 -> 13.9, 2 x 8 of 8000 8.8 -> 7.3;
+// below, 1 x 8 of 4000 5.8 -> 6.5.  grid = (n_splits * B, H_kv).
+constexpr int kFewStages = 4, kFewTokens = 16 * kFewStages;
 template <int P, bool N16, int QL>
-void launch(const Args& a, bool shared, hipStream_t s) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 && P == 4 ? 4 : 3))) void accumulate_weights_few(Args a) {
+    constexpr int kTileTokens = 4 * kFewTokens;
+    __shared__ __align__(16) uint8_t q_s[QL * 16 * 256];
+    __shared__ RowRule rule_s[16];
+    __shared__ float ref_s[16];
+    __shared__ int at_s[kD];
+    __shared__ int depth_s[64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, group = lane >> 4;
+    const Place place = place_at(a, blockIdx.x);
+    if (place.split < 0) return;
+    const int b = place.b, kvh = blockIdx.y;
+    StagedRows<P, QL, 16, 1> queries;
+    queries.request(a, b, kvh, 0);
+    const Seq s = sequence(a, b, place.len);
+    const int tiles = (s.len + kTileTokens - 1) / kTileTokens, last16 = (s.len - 1) & ~15;
+    if (place.split >= tiles) return;                            // (uniform for the workgroup)
+    const int64_t unit = (int64_t)b * a.H_kv + kvh;
+    const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
+    const ChunkAt whole = chunk_at<P, N16>(a, l16, group);
+    int lo_least, lo_most;
+    row_limits(a, s, b, 0, 16, lo_least, lo_most);
+    auto sees = [&](int t0) { return t0 < s.len && (t0 < s.prefix || t0 + kFewTokens > min(lo_least, max(s.base, 0))); };
+    Chunk<P, N16> raw[kFewStages];
+    float before;                                                // what the lane's token has so far
+    auto request = [&](int v) {                                  // (without a branch, as above)
+        int t0 = min(v, tiles - 1) * kTileTokens + wave * kFewTokens;
+        const int64_t mine = unit * a.w_stride + min(t0 + lane, s.len - 1);
+        before = *(a.w_in ? a.w_in + mine : a.lse_in);
+        t0 = sees(t0) ? t0 : last16;
+#pragma unroll
+        for (int st = 0; st < kFewStages; ++st) {
+            const int from = min(t0 + 16 * st, last16);
+            ChunkAt at = whole;
+            if (t0 + kFewTokens > s.len) at = chunk_at<P, N16>(a, min(t0 + 16 * st + l16, s.len - 1) - from, group);
+            load_chunk<P, N16>(a, a.k_mant, a.k_exp, stage_row(a, b, kvh, from), at, raw[st]);
+        }
+    };
+    request(place.split);
+    if (tid < 64) depth_s[tid] = tid < a.n_tok ? node_depth(node_mask(a, b, tid), tid) : 0;
+    if (tid < 16) {
+        rule_s[tid] = row_rule(a, s, b, kvh, tid);
+        ref_s[tid] = reference(a, b, kvh, tid);
+    }
+    queries.place(at_s);
+    lds_only_barrier();                                          // (the first cached rows are on their way)
+    queries.put(a, b, kvh, 0, q_s, at_s);
+    lds_only_barrier();
+    bf16x8 q[QL][4];
+#pragma unroll
+    for (int n = 0; n < QL; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[n][j] = staged_operand<16>(q_s, n, 0, l16, group, j);
+    const f32x4 ref = *(const f32x4*)(ref_s + 4 * group);
+    for (int v = place.split; v < tiles; v += place.n) {
+        const int t0 = v * kTileTokens + wave * kFewTokens;
+        if (t0 >= s.len) break;                                  // the wavefront's part of the last tile is empty
+        const bool seen = sees(t0), inner = t0 >= lo_most && t0 + kFewTokens <= s.base;
+        f32x4 sc[kFewStages];
+#pragma unroll
+        for (int st = 0; st < kFewStages; ++st) sc[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (seen) {
+#pragma unroll
+            for (int st = 0; st < kFewStages; ++st)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 k = __builtin_bit_cast(bf16x8, eight<P, N16>(raw[st], j));
+#pragma unroll
+                    for (int n = 0; n < QL; ++n) sc[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[n][j], k, sc[st], 0, 0, 0);
+                }
+        }
+        const float was = before;                                // (not multiplied before it is used: that would wait for it)
+        request(v + place.n);
+        float acc[kFewStages] = {};
+        if (seen && inner && a.cap == 0.f && !a.slopes) {
+#pragma unroll
+            for (int st = 0; st < kFewStages; ++st)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[st] += exp2_raw(fmaf(sc[st][i], mul, ref[i]));
+        } else if (seen) {
+            float y[4 * kFewStages];
+#pragma unroll
+            for (int i = 0; i < 4 * kFewStages; ++i) y[i] = sc[i >> 2][i & 3];
+            rule_tokens<kFewStages>(a, s, rule_s + 4 * group, depth_s, inner, t0 + l16, mul, y);
+#pragma unroll
+            for (int i = 0; i < 4 * kFewStages; ++i) acc[i >> 2] += exp2_raw(y[i] + ref[i & 3]);
+        }
+        const float got = groups_sum(acc);
+        if (t0 + lane < s.len) a.w_out[unit * a.w_stride + t0 + lane] = a.w_in ? fmaf(a.decay, was, got) : got;
+    }
+}
+
+enum Form { kFew, kTokens, kShared };
+template <int P, bool N16, int QL>
+void launch(const Args& a, Form form, hipStream_t s) {
     const dim3 grid((unsigned)(a.n_splits * a.batch), (unsigned)a.H_kv);
-    if (shared) accumulate_weights<P, N16, QL, true><<<grid, kThreads, 0, s>>>(a);
+    if (form == kFew) accumulate_weights_few<P, N16, QL><<<grid, kThreads, 0, s>>>(a);
+    else if (form == kShared) accumulate_weights<P, N16, QL, true><<<grid, kThreads, 0, s>>>(a);
     else accumulate_weights<P, N16, QL, false><<<grid, kThreads, 0, s>>>(a);
 }
 template <int P, bool N16>
-void launch(const Args& a, int dt, bool shared, hipStream_t s) {
-    if (dt == KVBFP_F32) launch<P, N16, 3>(a, shared, s);
-    else if (dt == KVBFP_F16) launch<P, N16, 2>(a, shared, s);
-    else launch<P, N16, 1>(a, shared, s);
+void launch(const Args& a, int dt, Form form, hipStream_t s) {
+    if (dt == KVBFP_F32) launch<P, N16, 3>(a, form, s);
+    else if (dt == KVBFP_F16) launch<P, N16, 2>(a, form, s);
+    else launch<P, N16, 1>(a, form, s);
 }
 
 }  // namespace
@@ -270,23 +378,26 @@ static int weights_impl(const char* call, const kvbfp_layout* L, const kvbfp_cac
     if (a.H_kv > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     a.perm_k = perm_k;
     a.lse_in = lse; a.w_in = weights_in; a.w_out = weights_out; a.w_stride = weights_stride; a.decay = decay;
-    // as many workgroups as the compute units have room for: three each, two with fp16 I/O
     const int64_t units = (int64_t)a.batch * a.H_kv;
-    int64_t tiles = (max_len + 4 * kWaveTokens - 1) / (4 * kWaveTokens);
-    const int64_t round = dtype == KVBFP_F16 ? 512 : 768;
-    const bool shared = a.M > 16 && tiles * units < round;
-    if (shared) tiles = (max_len + kWaveTokens - 1) / kWaveTokens;
+    const auto tiles_of = [&](int64_t tokens) { return (max_len + tokens - 1) / tokens; };
+    // as many workgroups as the compute units have room for
+    const int64_t few = dtype == KVBFP_BF16 && logical.mant_bits == 4 ? 1024 : 768, many = dtype == KVBFP_F16 ? 512 : 768;
+    const Form form = a.M <= 16 && tiles_of(4 * kFewTokens) * units >= 256 ? kFew
+                    : a.M > 16 && tiles_of(4 * kWaveTokens) * units < many    ? kShared
+                                                                               : kTokens;
+    const int64_t tiles = tiles_of(form == kFew ? 4 * kFewTokens : form == kShared ? kWaveTokens : 4 * kWaveTokens);
+    const int64_t round = form == kFew ? few : many;
     const bool shares = seq_len_dev && a.batch > 1 && a.batch <= 64;
     a.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles, round_of(round, units, shares)));
     a.share = shares && a.n_splits > 1;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool n16 = logical.block == 16;
     if (logical.mant_bits == 4) {
-        if (n16) launch<4, true>(a, (int)dtype, shared, s);
-        else launch<4, false>(a, (int)dtype, shared, s);
+        if (n16) launch<4, true>(a, (int)dtype, form, s);
+        else launch<4, false>(a, (int)dtype, form, s);
     } else {
-        if (n16) launch<8, true>(a, (int)dtype, shared, s);
-        else launch<8, false>(a, (int)dtype, shared, s);
+        if (n16) launch<8, true>(a, (int)dtype, form, s);
+        else launch<8, false>(a, (int)dtype, form, s);
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(KVBFP_ERR_HIP, "%s: %s", call, hipGetErrorString(err));

@@ -41,6 +41,17 @@ def test_ways_of_the_work(B, H, G, n, S, dtype):
     collect(case, False, 1.0, S)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("bits,block,page", [(4, 16, 0), (4, 128, 16), (8, 16, 32), (8, 32, 0)])
+def test_weights_of_few_rows_and_many_tokens(bits, block, page, dtype):
+    # 300 tiles of 256 tokens at least: lengths that end in every part of a tile
+    lens = [1, 15, 63, 64, 65, 128, 255, 256, 257, 300, 511, 513, 700, 767, 769, 800, 0, 801, 900, 1000]
+    for k, (G, n) in enumerate(((4, 1), (16, 1), (3, 5))):
+        extra = (dict(cap=20.0), dict(slopes=True, window=200), dict(tree=tree(k, n), prefix=[90] * 20))[k]
+        case = run_case(60 + k, 20, 4, G, n, 1000, bits, block, dtype, page=page, lens=lens, perm=True, **extra)
+        collect(case, k > 0, 0.9, 1000, in_place=k == 2)
+
+
 def test_all_empty_and_one_token():
     for B in (2, 64, 65):
         for n in (1, 20):
