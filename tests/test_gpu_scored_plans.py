@@ -122,3 +122,39 @@ def test_odd_addresses_of_the_output():
         odd = raw[1:1 + case["q"].numel()].view(case["q"].shape)
         kvbfp.decode_attention_scored(case["cache"], case["q"], S, case["scale"], out=odd, **args)
         assert torch.equal(odd, case["out"]) and raw[0] == -3 and (raw[1 + odd.numel():] == -3).all()
+
+
+def test_captured_weights_and_eviction_follow_the_inputs():
+    rng = np.random.default_rng(70)
+    B, H, S, keep = 16, 4, 1000, 300
+    cache, _ = R.make_cache(rng, B, H, S, 4, 32)
+    dst = kvbfp.alloc_cache(kvbfp.make_layout(D, 32, 4, H, B, keep), fill=0)
+    q = torch.from_numpy(rng.standard_normal((B, 1, H * 4, D)).astype(np.float32)).to(BF16).cuda()
+    lens, new_len = dev_i32(np.full(B, S)), torch.zeros(B, dtype=torch.int32, device="cuda")
+    lse, weights = torch.empty(B, 1, H * 4, device="cuda"), torch.zeros(B, H, S, device="cuda")
+    kept, left = torch.zeros(B, H, keep, dtype=torch.int32, device="cuda"), torch.zeros(B, H, keep, device="cuda")
+    ws = torch.empty(kvbfp.scored_workspace_bytes(cache.layout, H * 4, 1, S), dtype=torch.uint8, device="cuda")
+
+    def step():
+        kvbfp.decode_attention_scored(cache, q, S, 0.09, seq_len_dev=lens, lse=lse, workspace=ws)
+        kvbfp.accumulate_weights(cache, q, S, 0.09, lse, None, weights, seq_len_dev=lens)
+        kvbfp.evict(cache, dst, weights, S, keep, 4, 32, kept, new_len, weights_out=left, seq_len_dev=lens)
+
+    outputs = [weights, kept, left, new_len, *dst.planes()]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        lens.copy_(torch.from_numpy(rng.integers(0, S + 1, B).astype(np.int32)))
+        q.mul_(1.0 + 0.25 * k)
+        got = []
+        for run in (graph.replay, step):
+            for o in outputs:
+                o.zero_()
+            run()
+            torch.cuda.synchronize()
+            got.append([o.clone() for o in outputs])
+        assert all(torch.equal(a, b) for a, b in zip(*got)), k
+        assert torch.equal(new_len, lens.clamp(max=keep))
