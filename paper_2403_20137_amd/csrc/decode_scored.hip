@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 #pragma unroll
         for (int i = 0; i < N; ++i)                          // (by bits: a choice between elements of an array would go through memory)
             z[i] = RP == 16 ? y[0][i] : __uint_as_float((__float_as_uint(y[0][i & 3]) & ~second) | (__float_as_uint(y[0][4 + (i & 3)]) & second));
-        const float factor = rule_scores<N, QL == 3>(a, s, rule_s + row, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base,
+        const float factor = rule_scores<N>(a, s, rule_s + row, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base,
                                                      t0 + mine + 4 * group, mul, z);
         const float base = follow<N>(z, factor, slack, x[0], o[0]);
         uint32_t w[PL][N / 2];
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
             for (int c = 0; c < HC; ++c) {
                 uint32_t w[PL][4];
-                const float factor = rule_scores<8, QL == 3>(a, s, rule_s + 16 * (RW * c + rw) + l16, depth_s, inner, t0 + 4 * group, mul, y[c]);
+                const float factor = rule_scores<8>(a, s, rule_s + 16 * (RW * c + rw) + l16, depth_s, inner, t0 + 4 * group, mul, y[c]);
                 const float base = follow<8>(y[c], factor, slack, x[c], o[c]);
                 probabilities<PL, 8>(y[c], factor, base, x[c].sum, w);
 #pragma unroll

@@ -176,36 +176,33 @@ __device__ __forceinline__ RowRule row_rule(const Args& a, const Seq& s, int b, 
     return u;
 }
 
-// y = cap * tanh(y / cap) as cap - 2 cap / (1 + e^(2 y / cap)), off by up to 8 * 2^-24 of the cap.  A weight is then off by less than an eighth of
-// half a step of fp16 as long as the cap is at most kCapExp; larger caps and exact ones take the series to x^11 up to 0.35 (1.2e-8 relative),
-// where this form cancels, with one branch that asks on behalf of all N scores whether any is beyond.
-constexpr float kCapExp = 96.f;                // base 2: 8 * 2^-24 * 96 * ln 2 < 2^-14.9
-template <int N, bool EXACT>
+// y = cap * tanh(y / cap), x = y / cap.  Up to |x| = 0.9 as y + y x^2 q(x^2), q of degree 5 with the least largest error (1.6e-8 relative; with its roundings
+// 1.7 times 2^-24); beyond, where the difference cancels no more, as cap - 2 cap / (1 + e^(2 x)), within 6 times 2^-24 of the result.  That form alone for every
+// score is off by 4 times 2^-24 of the cap, twelve times as much as tanh in fp32 where scores are a fifteenth of it, and lse is an fp32 output.
+// One branch asks on behalf of all N scores whether any is beyond.
+template <int N>
 __device__ __forceinline__ void cap_scores(float (&y)[N], float mul, float cap, float inv_cap) {
-    auto by_exp = [&](float v, float turn) { return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + exp2_raw(v * turn)), cap); };
-    const float turn = inv_cap * 2.8853900817779268f;
-    if (!EXACT && cap <= kCapExp) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) y[i] = by_exp(y[i], mul * turn);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) y[i] *= mul;
     float most = 0.f, v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+        y[i] *= mul;
         const float x = y[i] * inv_cap, z = x * x;
-        float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
-        t = fmaf(z, t, -17.f / 315.f);
-        t = fmaf(z, t, 2.f / 15.f);
-        t = fmaf(z, t, -1.f / 3.f);
-        v[i] = fmaf(y[i] * z, t, y[i]);
+        float q = fmaf(z, 0.00130395917f, -0.00686005456f);
+        q = fmaf(z, q, 0.0209041256f);
+        q = fmaf(z, q, -0.0537214912f);
+        q = fmaf(z, q, 0.133303598f);
+        q = fmaf(z, q, -0.333332121f);
+        v[i] = fmaf(y[i] * z, q, y[i]);
         most = fmaxf(most, fabsf(x));
     }
-    constexpr float kSeries = 0.35f;
+    constexpr float kSeries = 0.9f;
     if (__builtin_amdgcn_ballot_w64(most > kSeries)) {
+        const float turn = inv_cap * 2.8853900817779268f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = fabsf(y[i] * inv_cap) > kSeries ? by_exp(y[i], turn) : v[i];
+        for (int i = 0; i < N; ++i) {
+            const float e = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + exp2_raw(y[i] * turn)), cap);
+            v[i] = fabsf(y[i] * inv_cap) > kSeries ? e : v[i];
+        }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = v[i];
@@ -215,12 +212,12 @@ __device__ __forceinline__ void cap_scores(float (&y)[N], float mul, float cap, 
 // plain scores; -inf where a token is not seen.  `inner`: all of them are seen, and are no nodes.  Returns what they are still to
 // be multiplied with: 1, or a positive `mul` that nothing has to come before, which costs nothing in the exponent's multiply-add.  The rule
 // lies in LDS: few tiles ask for it.
-template <int N, bool EXACT>
+template <int N>
 __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t0, float mul,
                                              float (&y)[N]) {
     float factor = 1.f;
     if (a.cap != 0.f) {
-        cap_scores<N, EXACT>(y, mul, a.cap, a.inv_cap);
+        cap_scores<N>(y, mul, a.cap, a.inv_cap);
     } else if (a.slopes || !(mul > 0.f)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) y[i] *= mul;
@@ -252,7 +249,7 @@ __device__ __forceinline__ float rule_scores(const Args& a, const Seq& s, const 
     return factor;
 }
 
-// The same for four rows (rule_s[0] ..) of the ST tokens t0 + 16 st, y[4 st + row], exactly; everything multiplied.
+// The same for four rows (rule_s[0] ..) of the ST tokens t0 + 16 st, y[4 st + row]; everything multiplied.
 template <int ST>
 __device__ __forceinline__ void rule_tokens(const Args& a, const Seq& s, const RowRule* rule_s, const int* depth_s, bool inner, int t0, float mul,
                                             float (&y)[4 * ST]) {
@@ -260,7 +257,7 @@ __device__ __forceinline__ void rule_tokens(const Args& a, const Seq& s, const R
 #pragma unroll
         for (int st = 0; st < ST; ++st) {
             float v[4] = {y[4 * st], y[4 * st + 1], y[4 * st + 2], y[4 * st + 3]};
-            cap_scores<4, true>(v, mul, a.cap, a.inv_cap);
+            cap_scores<4>(v, mul, a.cap, a.inv_cap);
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[4 * st + i] = v[i];
         }
