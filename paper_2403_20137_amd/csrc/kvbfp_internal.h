@@ -33,6 +33,13 @@ struct SplitPlan {
 constexpr int kTokenTile = 256;
 SplitPlan plan_splits(const kvbfp_layout* L, int32_t n_q_heads, int64_t max_len);
 
+// About what a call with a window reads of a sequence of `len` tokens for its last n_tok: the window's, and the first `prefix` (0 to len) of them.
+// At most len; nothing on the way passes 2^30 + 127 (lengths and prefixes reach 2^30, windows 63 more).
+constexpr int32_t tokens_read(int32_t len, int32_t window, int32_t n_tok, int32_t prefix) {
+    const int32_t near = window + n_tok < len ? window + n_tok : len;
+    return prefix < len - near ? near + prefix : len;
+}
+
 // A paged cache: `pool` describes the pool of pages (batch = pages, max_seq = tokens per page, a power of
 // two and at least kPageMin: the 16 tokens of a stage of the decode kernels never straddle two pages);
 // sequence b keeps tokens [i page, (i+1) page) in page block_table[b * table_stride + i].

@@ -75,7 +75,7 @@ __device__ __forceinline__ int length_of(const Args& a, int b) { return a.seq_le
 __device__ __forceinline__ void share_places(const Args& a, int lane, int& n, int& first, int& len) {
     len = length_of(a, min(lane, a.batch - 1));
     int read = len;                      // about what there is to read: documents are not looked at
-    if (a.window) read = min(len, a.window + a.n_tok + (a.prefix ? min(max(a.prefix[min(lane, a.batch - 1)], 0), len) : 0));
+    if (a.window) read = tokens_read(len, a.window, a.n_tok, a.prefix ? min(max(a.prefix[min(lane, a.batch - 1)], 0), len) : 0);
     const float mine = lane < a.batch ? (float)(read + 1) : 0.f;
     const float all = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wave_scan(mine)), 63));
     const float extra = (float)((a.n_splits - 1) * a.batch);
