@@ -225,6 +225,17 @@ def _stream_ptr(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _new(stream, make, *args, **kw):
+    """A tensor that a call makes itself, on the stream that its kernels run on: what fills it is done before them, and
+    its memory, given back before they have run, goes to nothing that does not come after them."""
+    if stream is None:
+        return make(*args, **kw)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_ptr(stream))
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 def _dev_ptr(t, dtype=None):
     if t is None:
         return None
@@ -342,8 +353,8 @@ def dequantize(cache: Cache, which, t0, n_tok, dtype=torch.float32, perm=None, o
     """DEVICE, async.  Returns [batch][n_tok][n_kv_heads][head_dim] of `dtype`."""
     L = cache.layout
     if out is None:
-        out = torch.empty((L.batch, n_tok, L.n_kv_heads, L.head_dim), dtype=dtype,
-                          device=cache.k_mant.device if cache.k_mant is not None else cache.v_mant.device)
+        out = _new(stream, torch.empty, (L.batch, n_tok, L.n_kv_heads, L.head_dim), dtype=dtype,
+                   device=cache.k_mant.device if cache.k_mant is not None else cache.v_mant.device)
     ptrs = cache.ptrs
     _check(lib().kvbfp_dequantize(C.byref(L), C.byref(ptrs), int(which), int(t0), int(n_tok),
                                   _dev_ptr(perm, torch.int32), _dev_ptr(out), _TORCH_DT[out.dtype],
@@ -355,25 +366,25 @@ def decode_workspace_bytes(layout: Layout, n_q_heads, max_len) -> int:
     return int(lib().kvbfp_decode_workspace_bytes(C.byref(layout), int(n_q_heads), int(max_len)))
 
 
-def _decode_common(cache, q, max_len, out, workspace):
+def _decode_common(cache, q, max_len, out, workspace, stream):
     L = cache.layout
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [batch][n_q_heads][head_dim] tensor")
     n_q_heads = q.shape[1]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if workspace is None:
         need = decode_workspace_bytes(L, n_q_heads, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     return L, n_q_heads, out, workspace
 
 
 def decode_attention(cache: Cache, q, max_len, softmax_scale, seq_len_dev=None, perm_k=None,
                      perm_v=None, out=None, workspace=None, stream=None):
     """DEVICE, async.  q: [batch][n_q_heads][head_dim] contiguous device tensor; returns `out`."""
-    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace, stream)
     ptrs = cache.ptrs
     _check(lib().kvbfp_decode_attention(C.byref(L), C.byref(ptrs), n_q_heads, _dev_ptr(q),
                                         _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32),
@@ -387,7 +398,7 @@ def decode_attention(cache: Cache, q, max_len, softmax_scale, seq_len_dev=None, 
 def decode_attention_qbfp(cache: Cache, q, max_len, softmax_scale, q_mant_bits, seq_len_dev=None, perm_k=None,
                           perm_v=None, out=None, workspace=None, stream=None):
     """DEVICE, async.  decode_attention with the permuted query cast to BFP (q_mant_bits 4 or 8) first."""
-    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace, stream)
     ptrs = cache.ptrs
     _check(lib().kvbfp_decode_attention_qbfp(C.byref(L), C.byref(ptrs), n_q_heads, _dev_ptr(q),
                                              _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32),
@@ -404,7 +415,7 @@ def decode_attention_rope(cache: Cache, q, max_len, softmax_scale, rope_theta, r
     """DEVICE, async (synchronous with profile=True).  Keys cached before the rotary embedding, rotated at
     read; rope_theta / rope_partner / rope_sign: device tensors [n_kv_heads][head_dim] (float32, int32,
     float32) as permute_rope returns them.  Returns `out`, or (out, split_ms, combine_ms) with profile."""
-    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace, stream)
     for t in (rope_theta, rope_partner, rope_sign):
         if t is None or tuple(t.shape) != (L.n_kv_heads, L.head_dim) or not t.is_contiguous():
             raise ValueError("rope_theta/rope_partner/rope_sign must be contiguous [n_kv_heads][head_dim] device tensors")
@@ -458,7 +469,7 @@ def dequantize_paged(pool: Cache, block_table, which, t0, n_tok, dtype=torch.flo
         raise ValueError("block_table must be a contiguous int32 device tensor [batch][pages per sequence]")
     batch = block_table.shape[0]
     if out is None:
-        out = torch.empty((batch, n_tok, L.n_kv_heads, L.head_dim), dtype=dtype, device=block_table.device)
+        out = _new(stream, torch.empty, (batch, n_tok, L.n_kv_heads, L.head_dim), dtype=dtype, device=block_table.device)
     ptrs = pool.ptrs
     _check(lib().kvbfp_dequantize_paged(C.byref(L), C.byref(ptrs), _dev_ptr(block_table, torch.int32), block_table.shape[1],
                                         batch, int(which), int(t0), int(n_tok), _dev_ptr(perm, torch.int32), _dev_ptr(out),
@@ -481,12 +492,12 @@ def decode_attention_paged(pool: Cache, block_table, q, max_len, softmax_scale, 
     _check_table(block_table, q.shape[0])
     n_q_heads = q.shape[1]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if workspace is None:
         need = decode_workspace_bytes_paged(L, block_table.shape[1], q.shape[0], n_q_heads, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     ptrs = pool.ptrs
     ms = (C.c_float * 2)() if profile else None
     _check(lib().kvbfp_decode_attention_paged(C.byref(L), C.byref(ptrs), _dev_ptr(block_table, torch.int32),
@@ -526,12 +537,12 @@ def append_decode_attention_paged(pool: Cache, block_table, k_new, v_new, q, max
     stride_b, stride_h = _new_row_strides(k_new, v_new, q.dtype, (q.shape[0], L.n_kv_heads, L.head_dim))
     n_q_heads = q.shape[1]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if workspace is None:
         need = decode_workspace_bytes_paged(L, block_table.shape[1], q.shape[0], n_q_heads, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     ptrs = pool.ptrs
     _check(lib().kvbfp_append_decode_attention_paged(
         C.byref(L), C.byref(ptrs), _dev_ptr(block_table, torch.int32), block_table.shape[1], q.shape[0], n_q_heads,
@@ -551,12 +562,12 @@ def decode_attention_multi_paged(pool: Cache, block_table, q, max_len, softmax_s
     _check_table(block_table, q.shape[0])
     n_tok, n_q_heads = q.shape[1], q.shape[2]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if workspace is None:
         need = decode_workspace_bytes_paged(L, block_table.shape[1], q.shape[0], n_q_heads * n_tok, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     ptrs = pool.ptrs
     _check(lib().kvbfp_decode_attention_multi_paged(
         C.byref(L), C.byref(ptrs), _dev_ptr(block_table, torch.int32), block_table.shape[1], q.shape[0], n_q_heads,
@@ -569,7 +580,7 @@ def decode_attention_multi_paged(pool: Cache, block_table, q, max_len, softmax_s
 def decode_attention_profile(cache: Cache, q, max_len, softmax_scale, q_mant_bits=0, seq_len_dev=None, perm_k=None,
                              perm_v=None, out=None, workspace=None, stream=None):
     """DEVICE, synchronous.  Same launches as decode_attention_qbfp; returns (out, split_ms, combine_ms)."""
-    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace, stream)
     ptrs = cache.ptrs
     ms = (C.c_float * 2)()
     _check(lib().kvbfp_decode_attention_profile(C.byref(L), C.byref(ptrs), n_q_heads, _dev_ptr(q),
@@ -585,7 +596,7 @@ def append_decode_attention(cache: Cache, k_new, v_new, q, max_len, softmax_scal
                             perm_v=None, q_mant_bits=0, out=None, workspace=None, stream=None):
     """DEVICE, async.  k_new / v_new: [batch][1][n_kv_heads][head_dim] (or [batch][n_kv_heads][head_dim]), the
     current token; stored at position seq_len - 1 (max_len - 1 without seq_len_dev), then attention."""
-    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(cache, q, max_len, out, workspace, stream)
     stride_b, stride_h = _new_row_strides(k_new, v_new, q.dtype, (L.batch, L.n_kv_heads, L.head_dim))
     ptrs = cache.ptrs
     _check(lib().kvbfp_append_decode_attention(C.byref(L), C.byref(ptrs), n_q_heads, _dev_ptr(k_new), _dev_ptr(v_new),
@@ -606,12 +617,12 @@ def decode_attention_multi(cache: Cache, q, max_len, softmax_scale, seq_len_dev=
         raise ValueError("q must be a contiguous [batch][n_q_tokens][n_q_heads][head_dim] tensor")
     n_tok, n_q_heads = q.shape[1], q.shape[2]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     if workspace is None:
         need = decode_workspace_bytes(L, n_q_heads * n_tok, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     ptrs = cache.ptrs
     _check(lib().kvbfp_decode_attention_multi(C.byref(L), C.byref(ptrs), n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype],
                                               _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
@@ -694,7 +705,7 @@ def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_
     rule = _check_rule(rule, batch, n_tok, n_q_heads)
     _check_lens(seq_len_dev, batch)
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(stream, torch.empty_like, q)
     else:
         _check_like_q(out, q)
     if lse is not None:
@@ -704,7 +715,7 @@ def _scored(cache, block_table, batch, q, max_len, softmax_scale, rule, seq_len_
             scored_workspace_bytes_paged(L, block_table.shape[1], batch, n_q_heads, n_tok, max_len)
         if need == 0:
             _check(ERR_INVALID_ARG)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device)
+        workspace = _new(stream, torch.empty, (need,), dtype=torch.uint8, device=q.device)
     ptrs = cache.ptrs
     rest = (n_q_heads, n_tok, _dev_ptr(q), _TORCH_DT[q.dtype], _dev_ptr(seq_len_dev, torch.int32), int(max_len), float(softmax_scale),
             _dev_ptr(perm_k, torch.int32), _dev_ptr(perm_v, torch.int32), rule, _dev_ptr(out), _dev_ptr(lse), _dev_ptr(workspace),
@@ -738,7 +749,8 @@ def _accumulate(cache, block_table, batch, q, max_len, softmax_scale, lse, weigh
     _check_lens(seq_len_dev, batch)
     _check_float(lse, "lse", shape[:3])
     if weights_out is None:
-        weights_out = torch.zeros((batch, L.n_kv_heads, max_len), dtype=torch.float32, device=q.device) if weights_in is None else weights_in
+        weights_out = weights_in if weights_in is not None else \
+            _new(stream, torch.zeros, (batch, L.n_kv_heads, max_len), dtype=torch.float32, device=q.device)
     size = weights_out.shape
     if len(size) != 3:
         raise ValueError("weights_out must be [batch][n_kv_heads][tokens]")
@@ -834,7 +846,7 @@ def measure_stream_read(cache: Cache, n_tok, wgs_per_unit=0, sink=None, stream=N
     """DEVICE, synchronous.  Plain read of rows [0, n_tok) of the four planes; returns the kernel time in ms."""
     L = cache.layout
     if sink is None:
-        sink = torch.zeros((4,), dtype=torch.uint8, device=cache.k_mant.device)
+        sink = _new(stream, torch.zeros, (4,), dtype=torch.uint8, device=cache.k_mant.device)
     ptrs = cache.ptrs
     ms = C.c_float(0)
     _check(lib().kvbfp_measure_stream_read(C.byref(L), C.byref(ptrs), int(n_tok), int(wgs_per_unit), _dev_ptr(sink),
@@ -846,7 +858,7 @@ def decode_attention_profile_ring(caches, n_launches, q, max_len, softmax_scale,
                                   perm_k=None, perm_v=None, out=None, workspace=None, stream=None):
     """DEVICE, synchronous.  The split pass n_launches times back to back over `caches` (a list of Cache objects of
     one layout, used cyclically), then the combine pass as often; returns (out, split_ms, combine_ms) per launch."""
-    L, n_q_heads, out, workspace = _decode_common(caches[0], q, max_len, out, workspace)
+    L, n_q_heads, out, workspace = _decode_common(caches[0], q, max_len, out, workspace, stream)
     arr = (CachePtrs * len(caches))(*[c.ptrs for c in caches])
     ms = (C.c_float * 2)()
     _check(lib().kvbfp_decode_attention_profile_ring(C.byref(L), arr, len(caches), int(n_launches), n_q_heads, _dev_ptr(q),
