@@ -468,8 +468,9 @@ typedef struct {
  *               run at the same time need one each.
  * seq_len_dev, max_len, perm_k, perm_v as in kvbfp_decode_attention.  Exponent planes at any address.  n_q_heads * n_q_tokens up to 65535.
  * Accumulation is fp32, the output is rounded once.  Range: cached blocks with exponent bytes 3 to 254 (4-bit mantissas) or 3 to 251
- * (8-bit) exactly, as kvbfp_decode_attention up to 32 heads; larger bytes are taken as the end of that range.  A bias is as exact as fp32:
- * relative to its own size (where every token that is seen is far away, what they differ by).
+ * (8-bit) exactly, however many of them stand at its upper end; larger bytes are taken as that end.  The scaled query as in
+ * kvbfp_decode_attention up to 32 heads.  A bias is as exact as fp32: relative to its own size (where every token that is seen is far away,
+ * what they differ by).
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
 size_t kvbfp_scored_workspace_bytes(const kvbfp_layout* layout, int32_t n_q_heads, int32_t n_q_tokens, int64_t max_len);
 int kvbfp_decode_attention_scored(const kvbfp_layout* layout, const kvbfp_cache* cache, int32_t n_q_heads, int32_t n_q_tokens,

@@ -90,22 +90,34 @@ __device__ __forceinline__ void add_values(ByChannel&& values, const bf16x8 (&p)
 
 // Running maximum of one row.  The sums are relative to a reference that scores may exceed by 2^kSlack before they are rescaled: 16 rows
 // have a new maximum nearly every tile otherwise, and 32 products each time.  Sums of values with exponent bytes up to kOrdinary have
-// room for that (below 2^74, times 2^kSlack, times 2^30 tokens); from the first larger byte on the reference is the maximum itself.
+// room for that (below 2^74, times 2^kSlack, times 2^30 tokens); from the first larger byte on no score may exceed the reference, and it rises above
+// the maximum with the sum of the weights: the largest values, as decoded, are below 2^122, so that weights of 2^6 in all fit.
 constexpr float kSlack = 8.f;
 constexpr uint32_t kOrdinary = 200;
 struct Running {
-    float ref = -INFINITY, most = -INFINITY, sum = 0.f;
+    float ref = -INFINITY, most = -INFINITY, sum = 0.f;       // (sum: of this lane's tokens, a quarter)
+    // After a tile with large values (weights of 32 at most): sums beyond 16 go down by 2^4, the reference up.
+    __device__ __forceinline__ void keep_room(f32x4 (&o)[8]) {
+        const bool full = rows_max(sum) > 4.f;
+        const float f = full ? 0x1p-4f : 1.f;
+        ref += full ? 4.f : 0.f;
+        sum *= f;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][i] *= f;
+    }
 };
-// Takes N scores (y times factor) into account; returns what they are taken relative to.
+// Takes N scores (y times factor, up to eight a lane) into account; returns what they are taken relative to.  `large`: there are such values.
 template <int N>
-__device__ __forceinline__ float follow(const float (&y)[N], float factor, float slack, Running& x, f32x4 (&o)[8]) {
+__device__ __forceinline__ float follow(const float (&y)[N], float factor, bool large, Running& x, f32x4 (&o)[8]) {
     float top = y[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, y[i]);
     x.most = fmaxf(x.most, rows_max(top * factor));
-    if (__builtin_amdgcn_ballot_w64(x.most > x.ref + slack)) {        // (the reference begins at minus infinity)
-        const float f = x.most > -INFINITY ? exp2_raw(x.ref - x.most) : 1.f;
-        x.ref = x.most;
+    if (__builtin_amdgcn_ballot_w64(x.most > x.ref + (large ? 0.f : kSlack))) {        // (the reference begins at minus infinity)
+        const float to = fmaxf(x.ref, x.most), f = to > -INFINITY ? exp2_raw(x.ref - to) : 1.f;
+        x.ref = to;
         x.sum *= f;
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct)
@@ -185,22 +197,26 @@ __device__ __forceinline__ int64_t out_row(const Args& a, int b, int kvh, int r)
     return ((int64_t)b * a.n_tok + tok) * a.H_q + (int64_t)kvh * a.G + (r - tok * a.G);
 }
 
+// Up to 8 times 768 parts are joined: sums with large values, whose weights are 2^5.6 at most in all, are joined 2^-16 times, and handed on so with a
+// reference 16 higher.
+constexpr float kDown = 0x1p-16f, kUp = 0x1p16f;
+
 // Partial results of a wavefront's own 16 rows from r0 on.
-__device__ __forceinline__ void store_partial(const Args& a, int kvh, int r0, int place, int lane, const f32x4 (&o)[8], const Running& x) {
+__device__ __forceinline__ void store_partial(const Args& a, int kvh, int r0, int place, int lane, const f32x4 (&o)[8], const Running& x, bool large) {
     const int l16 = lane & 15, group = lane >> 4, r = r0 + l16;
-    const float sum = rows_sum(x.sum);
+    const float sum = rows_sum(x.sum), by = large ? kDown : 1.f;
     if (r >= a.M) return;
     const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
 #pragma unroll
-    for (int ct = 0; ct < 8; ++ct) *(f32x4*)(a.part_o + at * kD + 16 * ct + 4 * group) = o[ct];
-    if (group == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(x.ref, sum);
+    for (int ct = 0; ct < 8; ++ct) *(f32x4*)(a.part_o + at * kD + 16 * ct + 4 * group) = o[ct] * by;
+    if (group == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(large ? x.ref + 16.f : x.ref, sum * by);
 }
 // The sums of a workgroup's wavefronts for RP * RW rows from r0 on, joined over the 4 / RW that hold the same rows (wavefront w: rows
 // 16 (w % RW) .., or twice the same 8 rows, RP = 8, RW = 1) and written as this split's partial result, or as the output
 // where there is one split.  smem: four times kWaveLds, free when this is called.
 template <int P, int QL, int RW, int RP>
 __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, int place, uint8_t* smem, float (*ml_s)[16][2], int wave, int lane,
-                                       const f32x4 (&o)[8], const Running& x) {
+                                       const f32x4 (&o)[8], const Running& x, bool large) {
     const int tid = threadIdx.x, l16 = lane & 15, group = lane >> 4;
     constexpr float up = (float)(1 << Decode<P>::kShift);       // (partial results keep the scale of the decoded values)
     float* const o_s = (float*)(smem + wave * kWaveLds);
@@ -209,7 +225,7 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
     const float sum = rows_sum(x.sum);
     if (group == 0) {
         ml_s[wave][l16][0] = x.ref;
-        ml_s[wave][l16][1] = sum;
+        ml_s[wave][l16][1] = large ? -sum : sum;             // (the sign says so)
     }
     const int row = tid >> 4, p0 = (tid & 15) * 8;
     int channel[8];
@@ -225,11 +241,16 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
     for (int rw = 0; rw < RW; ++rw) {
         const int r = r0 + 16 * rw + row;
         if (row >= RP || r >= a.M) continue;
-        float top = -INFINITY, den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        float top = -INFINITY, least = 0.f, den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = rw; w < 4; w += RW)
 #pragma unroll
-            for (int h = 0; h < 16; h += RP) top = fmaxf(top, ml_s[w][(row + h) & 15][0]);
+            for (int h = 0; h < 16; h += RP) {
+                top = fmaxf(top, ml_s[w][(row + h) & 15][0]);
+                least = fminf(least, ml_s[w][(row + h) & 15][1]);
+            }
+        const bool any_large = least < 0.f;
+        const float down = any_large ? kDown : 1.f;
 #pragma unroll
         for (int w = rw; w < 4; w += RW) {
 #pragma unroll
@@ -237,22 +258,23 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
                 const int at = (row + h) & 15;
                 if (!(ml_s[w][at][0] > -INFINITY)) continue;
                 const float f = exp2_raw(ml_s[w][at][0] - top);
-                den = fmaf(f, ml_s[w][at][1], den);
+                den = fmaf(f, fabsf(ml_s[w][at][1]), den);
                 const float* const src = (const float*)(smem + w * kWaveLds) + at * kOStride + p0;
+                const float f_o = f * down;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] = fmaf(f, src[i], acc[i]);
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(f_o, src[i], acc[i]);
             }
         }
         if (a.n_splits > 1) {
             const int64_t at = ((int64_t)kvh * a.M + r) * a.n_splits * a.batch + place;
-            if (p0 == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(top, den);
+            if (p0 == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(any_large ? top + 16.f : top, den * down);
             *(f32x4*)(a.part_o + at * kD + p0) = f32x4{acc[0], acc[1], acc[2], acc[3]};
             *(f32x4*)(a.part_o + at * kD + p0 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
         } else {
             // into the order of the output in LDS, where the row came from (nobody but these 16 lanes looks at it): stores of single
             // channels took longer than everything before them with 108 rows of two tokens, 23 us against 18.7
             const int64_t at = out_row(a, b, kvh, r);
-            const float by = den > 0.f ? up / den : 0.f;
+            const float by = den > 0.f ? up / den * (any_large ? kUp : 1.f) : 0.f;
             float* const row_s = (float*)(smem + rw * kWaveLds) + row * kOStride;
             wave_fence();
 #pragma unroll
@@ -324,7 +346,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
     uint8_t* const v_s = smem + wave * kWaveLds;
     f32x4 o[1][8];
     Running x[1];
-    float slack = kSlack;
+    bool large = false;
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) o[0][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float mul = a.score_mul * (float)(1 << Decode<P>::kShift);
@@ -342,7 +364,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 *(u32x4*)(v_s + value_at(16 * st + l16, 2 * group + (j >> 1), j & 1)) = eight<P, N16>(vc[st], j);
-        if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) slack = 0.f;
+        if (__builtin_amdgcn_ballot_w64(has_large(vc[0]) || has_large(vc[1]))) large = true;
         wave_fence();
         constexpr int N = RP / 2;
         float z[N];
@@ -351,7 +373,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             z[i] = RP == 16 ? y[0][i] : __uint_as_float((__float_as_uint(y[0][i & 3]) & ~second) | (__float_as_uint(y[0][4 + (i & 3)]) & second));
         const float factor = rule_scores<N>(a, s, rule_s + row, depth_s, t0 >= lo_most && t0 + kWaveTokens <= s.base,
                                                      t0 + mine + 4 * group, mul, z);
-        const float base = follow<N>(z, factor, slack, x[0], o[0]);
+        const float base = follow<N>(z, factor, large, x[0], o[0]);
         uint32_t w[PL][N / 2];
         probabilities<PL, N>(z, factor, base, x[0].sum, w);
         bf16x8 p[1][PL];
@@ -363,10 +385,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 
             p[0][i] = __builtin_bit_cast(bf16x8, v);
         }
         add_values<PL, 1>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
+        if (large) x[0].keep_room(o[0]);
         wave_fence();
     }
     __syncthreads();
-    finish<P, QL, 1, RP>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
+    finish<P, QL, 1, RP>(a, b, kvh, 0, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0], large);
 }
 
 // More rows: a workgroup decodes 64 tokens at a time to bf16 in LDS, once for all its rows.  RW wavefronts have HC times 16 rows each
@@ -454,13 +477,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         request(after(place.split));
     }
     int half = 0;
-    float slack = kSlack;
+    bool large = false;
     for (int v = place.split; v < tiles.count; v += n_splits, half ^= 1) {
         lds_only_barrier();                                  // this tile is complete; the one before it is not looked at any more
         const uint8_t* const tile = smem + half * kTile;
         if (v + n_splits < tiles.count) decode(half ^ 1);
         request(after(after(v)));
-        if (large_s[half]) slack = 0.f;
+        if (__builtin_amdgcn_readfirstlane(large_s[half])) large = true;
         // 32 tokens at a time, not unrolled: the registers of two steps together do not fit.  With 16 rows a wavefront the values and the
         // next keys are read ahead of the softmax, whose instructions then fill the time of the reads.
         bf16x8 k[2][4];
@@ -493,7 +516,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             for (int c = 0; c < HC; ++c) {
                 uint32_t w[PL][4];
                 const float factor = rule_scores<8>(a, s, rule_s + 16 * (RW * c + rw) + l16, depth_s, inner, t0 + 4 * group, mul, y[c]);
-                const float base = follow<8>(y[c], factor, slack, x[c], o[c]);
+                const float base = follow<8>(y[c], factor, large, x[c], o[c]);
                 probabilities<PL, 8>(y[c], factor, base, x[c].sum, w);
 #pragma unroll
                 for (int i = 0; i < PL; ++i) p[c][i] = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i][2], w[i][3]});
@@ -501,16 +524,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             __builtin_amdgcn_s_setprio(1);
             if (HC == 1) add_values<PL, HC>([&](int ct) { return by_channel.v[ct]; }, p, o);
             else add_values<PL, HC>([&](int ct) { return values_of(v_s, lane, ct); }, p, o);
+            if (large) {
+#pragma unroll
+                for (int c = 0; c < HC; ++c) x[c].keep_room(o[c]);
+            }
         }
     }
 #pragma unroll 1
     for (int c = 0;; ++c) {                                  // (a loop: code that runs once is as long as its way from memory)
         const int rc = r0 + 16 * RW * c;
         if (RW == 4 && a.n_splits > 1) {                     // nothing to join
-            store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[0], x[0]);
+            store_partial(a, kvh, rc + 16 * wave, blockIdx.x, lane, o[0], x[0], large);
         } else {
             __syncthreads();
-            finish<P, QL, RW, 16>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0]);
+            finish<P, QL, RW, 16>(a, b, kvh, rc, blockIdx.x, smem, ml_s, wave, lane, o[0], x[0], large);
         }
         if (c == HC - 1 || rc + 16 * RW >= a.M) break;
 #pragma unroll

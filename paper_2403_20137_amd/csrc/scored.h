@@ -26,7 +26,7 @@ struct Args {
     const int32_t* perm_k;     // [H_kv][D] or nullptr
     const int32_t* perm_v;
     float* part_o;             // [H_kv][M][n_splits * B][D], in the order of the positions in LDS (see position_channel)
-    float* part_ml;            // [H_kv][M][n_splits * B][2]: largest score (base 2), sum of the weights relative to it
+    float* part_ml;            // [H_kv][M][n_splits * B][2]: reference (base 2), sum of the weights relative to it
     const int32_t* block_table;
     int64_t table_stride, max_seq;
     int32_t log2_page, n_pages;
