@@ -462,11 +462,13 @@ typedef struct {
 /* DEVICE, asynchronous.  Attention for the last n_q_tokens tokens of every sequence with a rule on the scores: kvbfp_decode_attention_multi
  * (the same products and layouts, 1..64 query tokens that are cached already) with a tree of drafted tokens in place of the causal order,
  * capped or biased scores, windows, documents, prefixes.  rule = NULL is that call's causal order.
- *   q, out    : DEVICE [batch][n_q_tokens][n_q_heads][head_dim] of `dtype`, contiguous.
+ *   q, out    : DEVICE [batch][n_q_tokens][n_q_heads][head_dim] of `dtype`, contiguous.  out may be q itself.
  *   lse       : DEVICE float [batch][n_q_tokens][n_q_heads] or NULL: the natural logarithm of the sum of exp(y) over the tokens seen.
  *   workspace : DEVICE, at least kvbfp_scored_workspace_bytes(layout, n_q_heads, n_q_tokens, max_len) bytes, 256-byte aligned.  Calls that may
  *               run at the same time need one each.
  * seq_len_dev, max_len, perm_k, perm_v as in kvbfp_decode_attention.  Exponent planes at any address.  n_q_heads * n_q_tokens up to 65535.
+ * Here and in the two calls below every array is aligned to its elements, and what a call writes shares no byte with anything else that it is
+ * given, but for what is said of it (INVALID_ARG otherwise).
  * Accumulation is fp32, the output is rounded once.  Range: cached blocks with exponent bytes 3 to 254 (4-bit mantissas) or 3 to 251
  * (8-bit) exactly, however many of them stand at its upper end; larger bytes are taken as that end.  The scaled query as in
  * kvbfp_decode_attention up to 32 heads.  A bias is as exact as fp32: relative to its own size (where every token that is seen is far away,

@@ -771,6 +771,24 @@ int fill_args(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache,
     return KVBFP_OK;
 }
 
+int check_arrays(const char* call, const kvbfp_layout* L, const Args& a, size_t element, std::initializer_list<Span> written) {
+    size_t m, e;
+    if (int rc = kvbfp_cache_bytes(L, &m, &e)) return rc;
+    const size_t batch = (size_t)a.batch, rows = batch * (size_t)a.n_tok * (size_t)a.H_q, perm = (size_t)a.H_kv * kD * sizeof(int32_t);
+    return check_spans(call, written,
+                       {{"k_mant", a.k_mant, m}, {"k_exp", a.k_exp, e}, {"v_mant", a.v_mant, m}, {"v_exp", a.v_exp, e},
+                        {"q", a.q == a.out ? nullptr : a.q, rows * kD * element, element},
+                        {"lse", a.lse_in, rows * sizeof(float), sizeof(float)},
+                        {"weights_in", a.w_in == a.w_out ? nullptr : a.w_in, batch * (size_t)a.H_kv * (size_t)a.w_stride * sizeof(float), sizeof(float)},
+                        {"seq_len_dev", a.seq_len, batch * sizeof(int32_t), sizeof(int32_t)},
+                        {"perm_k", a.perm_k, perm, sizeof(int32_t)}, {"perm_v", a.perm_v, perm, sizeof(int32_t)},
+                        {"block_table", a.block_table, batch * (size_t)a.table_stride * sizeof(int32_t), sizeof(int32_t)},
+                        {"rule.slopes", a.slopes, (size_t)a.H_q * sizeof(float), sizeof(float)},
+                        {"rule.first_dev", a.first, batch * (size_t)a.n_tok * sizeof(int32_t), sizeof(int32_t)},
+                        {"rule.prefix_dev", a.prefix, batch * sizeof(int32_t), sizeof(int32_t)},
+                        {"rule.tree_mask", a.tree, ((batch - 1) * (size_t)a.tree_stride + (size_t)a.n_tok) * sizeof(uint64_t), sizeof(uint64_t)}});
+}
+
 }  // namespace scored
 }  // namespace kvbfp
 
@@ -801,6 +819,10 @@ static int scored_impl(const char* call, const kvbfp_layout* L, const kvbfp_cach
         a.part_o = (float*)workspace;
         a.part_ml = a.part_o + (size_t)a.batch * a.H_kv * a.M * a.n_splits * kD;
     }
+    const size_t rows = (size_t)a.batch * (size_t)a.n_tok * (size_t)a.H_q, element = (size_t)dtype_size(dtype);
+    if (int rc = check_arrays(call, L, a, element, {{"out", out, rows * kD * element, element}, {"lse", lse, rows * sizeof(float), sizeof(float)},
+                                                    {"workspace", need ? workspace : nullptr, need}}))
+        return rc;
     hipStream_t s = (hipStream_t)hip_stream;
     if (logical.mant_bits == 4) launch_split<4>(a, (int)dtype, p, s);
     else launch_split<8>(a, (int)dtype, p, s);

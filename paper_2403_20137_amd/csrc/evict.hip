@@ -264,11 +264,6 @@ __global__ __launch_bounds__(256) void evict_rows(EvictArgs a) {
 
 using namespace kvbfp;
 
-// The planes of a cache that may be written and read share no byte.
-static bool overlap(const void* p, size_t n, const void* q, size_t m) {
-    return (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n;
-}
-
 static int evict_impl(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache, const Paging* paging, const kvbfp_layout* dst_L,
                       const kvbfp_cache* dst, const Paging* dst_paging, const float* weights, int64_t weights_stride,
                       const int32_t* seq_len_dev, int64_t max_len, int32_t n_keep, int32_t n_first, int32_t n_recent, int32_t* kept,
@@ -300,24 +295,28 @@ static int evict_impl(const char* call, const kvbfp_layout* L, const kvbfp_cache
     if (from.batch > 65535 || from.n_kv_heads > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: batch/heads exceed the grid limits", call);
     const void* const p[4] = {cache->k_mant, cache->k_exp, cache->v_mant, cache->v_exp};
     const void* const q[4] = {dst->k_mant, dst->k_exp, dst->v_mant, dst->v_exp};
-    if (paging && std::equal(p, p + 4, q)) {               // other pages of one pool
-        if (L->max_seq != dst_L->max_seq || L->batch != dst_L->batch)
-            return fail(KVBFP_ERR_INVALID_ARG, "%s: one pool with two layouts", call);
-    } else {
-        size_t m[2], e[2];
-        if (int rc = kvbfp_cache_bytes(L, &m[0], &e[0])) return rc;
-        if (int rc = kvbfp_cache_bytes(dst_L, &m[1], &e[1])) return rc;
-        for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j)
-                if (overlap(p[i], i & 1 ? e[0] : m[0], q[j], j & 1 ? e[1] : m[1]))
-                    return fail(KVBFP_ERR_INVALID_ARG, "%s: the two caches overlap", call);
-    }
-    // lengths and weights are read beside the writing of the new ones
-    const size_t units = (size_t)from.batch * (size_t)from.n_kv_heads;
-    if (seq_len_dev && overlap(seq_len_dev, from.batch * sizeof(int32_t), new_len, from.batch * sizeof(int32_t)))
-        return fail(KVBFP_ERR_INVALID_ARG, "%s: new_len overlaps seq_len_dev", call);
-    if (weights_out && overlap(weights, units * (size_t)weights_stride * sizeof(float), weights_out, units * (size_t)n_keep * sizeof(float)))
-        return fail(KVBFP_ERR_INVALID_ARG, "%s: weights_out overlaps weights", call);
+    const bool one_pool = paging && std::equal(p, p + 4, q);                 // other pages of it
+    if (one_pool && (L->max_seq != dst_L->max_seq || L->batch != dst_L->batch))
+        return fail(KVBFP_ERR_INVALID_ARG, "%s: one pool with two layouts", call);
+    // what is read and what is written, at the same time
+    size_t m[2], e[2];
+    if (int rc = kvbfp_cache_bytes(L, &m[0], &e[0])) return rc;
+    if (int rc = kvbfp_cache_bytes(dst_L, &m[1], &e[1])) return rc;
+    const size_t units = (size_t)from.batch * (size_t)from.n_kv_heads, kept_bytes = units * (size_t)n_keep * sizeof(int32_t),
+                 lens = (size_t)from.batch * sizeof(int32_t);
+    const auto source = [&](int i) { return Span{"the first cache", one_pool ? nullptr : p[i], i & 1 ? e[0] : m[0]}; };
+    const auto table = [&](const char* what, const Paging* pg) {
+        return Span{what, pg ? pg->block_table : nullptr, pg ? lens * (size_t)pg->table_stride : 0, sizeof(int32_t)};
+    };
+    if (int rc = check_spans(call,
+                             {{"kept", kept, kept_bytes, sizeof(int32_t)}, {"new_len", new_len, lens, sizeof(int32_t)},
+                              {"weights_out", weights_out, kept_bytes, sizeof(float)},
+                              {"the second cache", q[0], m[1]}, {"the second cache", q[1], e[1]},
+                              {"the second cache", q[2], m[1]}, {"the second cache", q[3], e[1]}},
+                             {{"weights", weights, units * (size_t)weights_stride * sizeof(float), sizeof(float)},
+                              {"seq_len_dev", seq_len_dev, lens, sizeof(int32_t)}, table("block_table", paging), table("dst_table", dst_paging),
+                              source(0), source(1), source(2), source(3)}))
+        return rc;
     EvictArgs a{};
     a.src[0] = cache->k_mant; a.src[1] = cache->k_exp; a.src[2] = cache->v_mant; a.src[3] = cache->v_exp;
     a.dst[0] = dst->k_mant; a.dst[1] = dst->k_exp; a.dst[2] = dst->v_mant; a.dst[3] = dst->v_exp;

@@ -55,6 +55,22 @@ int check_cache(const kvbfp_cache* c, bool need_k, bool need_v) {
     return KVBFP_OK;
 }
 
+int check_spans(const char* call, std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    for (const auto* list : {&written, &read})
+        for (const Span& x : *list)
+            if ((uintptr_t)x.at % x.element != 0) return fail(KVBFP_ERR_INVALID_ARG, "%s: %s is not aligned to its elements", call, x.what);
+    const auto meet = [](const Span& x, const Span& y) {
+        return x.at && y.at && (uintptr_t)x.at < (uintptr_t)y.at + y.bytes && (uintptr_t)y.at < (uintptr_t)x.at + x.bytes;
+    };
+    for (const Span* x = written.begin(); x != written.end(); ++x) {
+        for (const Span* y = x + 1; y != written.end(); ++y)
+            if (meet(*x, *y)) return fail(KVBFP_ERR_INVALID_ARG, "%s: %s and %s overlap", call, x->what, y->what);
+        for (const Span& y : read)
+            if (meet(*x, y)) return fail(KVBFP_ERR_INVALID_ARG, "%s: %s overlaps %s", call, x->what, y.what);
+    }
+    return KVBFP_OK;
+}
+
 int check_paging(const kvbfp_layout* pool, const Paging& pg, kvbfp_layout* logical) {
     if (int rc = check_device_layout(pool)) return rc;
     if (!pg.block_table) return fail(KVBFP_ERR_INVALID_ARG, "paged cache: block_table is NULL");

@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 
 #include "kvbfp.h"
 
@@ -25,6 +26,16 @@ inline int dtype_size(int dtype) {
 // Checks the layout for the device kernels; returns KVBFP_OK or records an error.
 int check_device_layout(const kvbfp_layout* L);
 int check_cache(const kvbfp_cache* c, bool need_k, bool need_v);
+
+// Arrays of a call (NULL: not given).  Those that it writes must share no byte with each other or with what it reads, and all must be aligned
+// to their elements.
+struct Span {
+    const char* what;
+    const void* at;
+    size_t bytes;
+    size_t element = 1;
+};
+int check_spans(const char* call, std::initializer_list<Span> written, std::initializer_list<Span> read);
 
 // Number of splits (partial results per query head) decode attention uses for this geometry.
 struct SplitPlan {

@@ -470,6 +470,8 @@ __device__ __forceinline__ void query_operand(const float* q_s, const int* perm_
 int fill_args(const char* call, const kvbfp_layout* L, const kvbfp_cache* cache, const Paging* paging, int32_t n_q_heads, int32_t n_q_tokens,
               const void* q, kvbfp_dtype dtype, const int32_t* seq_len_dev, int64_t max_len, float softmax_scale,
               const kvbfp_score_rule* rule, bool need_v, Args* a, kvbfp_layout* logical);
+// What the call reads, as `a` has it by now, against what it writes.
+int check_arrays(const char* call, const kvbfp_layout* L, const Args& a, size_t element, std::initializer_list<Span> written);
 
 }  // namespace scored
 }  // namespace kvbfp

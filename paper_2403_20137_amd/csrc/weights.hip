@@ -378,6 +378,7 @@ static int weights_impl(const char* call, const kvbfp_layout* L, const kvbfp_cac
     if (a.H_kv > 65535) return fail(KVBFP_ERR_UNSUPPORTED, "%s: too many heads for the grid", call);
     a.perm_k = perm_k;
     a.lse_in = lse; a.w_in = weights_in; a.w_out = weights_out; a.w_stride = weights_stride; a.decay = decay;
+    if (int rc = check_arrays(call, L, a, (size_t)dtype_size(dtype), {{"weights_out", weights_out, bytes, sizeof(float)}})) return rc;
     const int64_t units = (int64_t)a.batch * a.H_kv;
     const auto tiles_of = [&](int64_t tokens) { return (max_len + tokens - 1) / tokens; };
     // as many workgroups as the compute units have room for
