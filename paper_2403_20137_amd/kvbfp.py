@@ -640,10 +640,18 @@ def _rule_tensor(t, what, dtype, dims):
     return _dev_ptr(t)
 
 
+def _int32(x, what):
+    """ctypes would cut it to 32 bits without a word."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError("%s = %d does not fit 32 bits" % (what, x))
+    return x
+
+
 def make_score_rule(cap=0.0, slopes=None, window=0, first_dev=None, prefix_dev=None, tree_mask=None) -> ScoreRule:
     """Rule on the scores (kvbfp_score_rule).  slopes: float32 [n_q_heads]; first_dev: int32 [batch][n_q_tokens]; prefix_dev: int32
     [batch]; tree_mask: int64 (64 bits) [batch][n_q_tokens], or [n_q_tokens] for one tree for all.  Holds its tensors."""
-    r = ScoreRule(C.sizeof(ScoreRule), float(cap), int(window), 0, _rule_tensor(slopes, "slopes", torch.float32, (1,)),
+    r = ScoreRule(C.sizeof(ScoreRule), float(cap), _int32(window, "window"), 0, _rule_tensor(slopes, "slopes", torch.float32, (1,)),
                   _rule_tensor(first_dev, "first_dev", torch.int32, (2,)), _rule_tensor(prefix_dev, "prefix_dev", torch.int32, (1,)),
                   _rule_tensor(tree_mask, "tree_mask", torch.int64, (1, 2)))
     if tree_mask is not None and tree_mask.dim() == 2:
@@ -795,7 +803,8 @@ def _evict_args(batch, heads, weights, max_len, n_keep, n_first, n_recent, kept,
     if weights_out is not None:
         _check_float(weights_out, "weights_out", (batch, heads, n_keep))
     _check_lens(seq_len_dev, batch)
-    return (_dev_ptr(weights), size[2], _dev_ptr(seq_len_dev, torch.int32), int(max_len), int(n_keep), int(n_first), int(n_recent),
+    return (_dev_ptr(weights), size[2], _dev_ptr(seq_len_dev, torch.int32), int(max_len), _int32(n_keep, "n_keep"), _int32(n_first, "n_first"),
+            _int32(n_recent, "n_recent"),
             _dev_ptr(kept, torch.int32), _dev_ptr(new_len, torch.int32), _dev_ptr(weights_out), _stream_ptr(stream))
 
 
