@@ -493,7 +493,8 @@ int kvbfp_decode_attention_scored_paged(const kvbfp_layout* pool, const kvbfp_ca
 /* DEVICE, asynchronous.  The attention weights that cached tokens collect, per kv-head:
  *     weights_out[b][h][t] = decay * weights_in[b][h][t] + sum over the query tokens i and the query heads of kv-head h of exp(y - lse)
  * with y and the tokens seen as kvbfp_decode_attention_scored has them and the lse that it returned for the same q, rule, scale and
- * lengths (a row whose lse is -infinity adds nothing).  Reads the keys alone, once.
+ * lengths (a row whose lse is -infinity adds nothing).  Reads the keys alone, once for every 128 rows of a kv-head (query tokens times heads
+ * of its group; 64 with fp32 I/O), and from the second time on the weights that it has written so far.
  *   lse         : DEVICE float [batch][n_q_tokens][n_q_heads].
  *   weights_in  : DEVICE float [batch][n_kv_heads][weights_stride], or NULL = zeros (decay is then not looked at).
  *   weights_out : DEVICE, the same shape; may be weights_in itself (but not overlap it otherwise).  Tokens from seq_len on are left as they are.
