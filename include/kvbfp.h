@@ -496,7 +496,8 @@ int kvbfp_decode_attention_scored_paged(const kvbfp_layout* pool, const kvbfp_ca
  * lengths (a row whose lse is -infinity adds nothing).  Reads the keys alone, once for every 128 rows of a kv-head (query tokens times heads
  * of its group; 64 with fp32 I/O), and from the second time on the weights that it has written so far.
  *   lse         : DEVICE float [batch][n_q_tokens][n_q_heads].
- *   weights_in  : DEVICE float [batch][n_kv_heads][weights_stride], or NULL = zeros (decay is then not looked at).
+ *   weights_in  : DEVICE float [batch][n_kv_heads][weights_stride], or NULL = zeros.
+ *   decay       : finite, also without weights_in, where it has no effect.
  *   weights_out : DEVICE, the same shape; may be weights_in itself (but not overlap it otherwise).  Tokens from seq_len on are left as they are.
  *   cache       : the value planes may be NULL.
  * No atomics: the same bits every time.  Errors: INVALID_ARG (also weights_stride < max_len), UNSUPPORTED, HIP. */
