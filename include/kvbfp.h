@@ -514,7 +514,9 @@ int kvbfp_accumulate_weights_paged(const kvbfp_layout* pool, const kvbfp_cache* 
 /* DEVICE, asynchronous.  Eviction by collected weight: of every sequence and kv-head the first n_first tokens, the last n_recent and, of those
  * between them, the ones with the largest weights stay, n_keep in all (a sequence of up to n_keep tokens stays whole), and go in their
  * order to rows 0, 1, .. of another cache, bit for bit.  Equal weights: the lower index stays; NaN counts below everything.
- * Keys are taken as they are: rotated before they were cached, they keep the angles of their old positions.
+ * Keys are taken as they are: rotated before they were cached, they keep the angles of their old positions.  Positions are not kept either, and
+ * heads keep different tokens: to a score rule the rows that stay lie side by side, so that its slopes, window, first tokens and prefix mean
+ * distances and places among these.  A tree or a causal order among the last tokens is not touched where n_recent holds them, nor is a cap.
  *   dst_layout, dst : the other cache (same block, mant_bits, n_kv_heads, batch; max_seq >= n_keep); must not overlap the first.  Rows
  *                     from the new length on are left as they are.
  *   weights     : DEVICE float [batch][n_kv_heads][weights_stride], as kvbfp_accumulate_weights leaves them.
