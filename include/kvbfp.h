@@ -469,8 +469,8 @@ typedef struct {
  * seq_len_dev, max_len, perm_k, perm_v as in kvbfp_decode_attention.  Exponent planes at any address.  n_q_heads * n_q_tokens up to 65535.
  * Here and in the two calls below every array is aligned to its elements, and what a call writes shares no byte with anything else that it is
  * given, but for what is said of it (INVALID_ARG otherwise).
- * Accumulation is fp32, the output is rounded once.  Range: cached blocks with exponent bytes 3 to 254 (4-bit mantissas) or 3 to 251
- * (8-bit) exactly, however many of them stand at its upper end; larger bytes are taken as that end.  The scaled query as in
+ * Scores, lse and sums are fp32; a probability enters the value product with 16 bits with 16-bit I/O, with 24 otherwise; the output is rounded
+ * once.  Range: cached blocks with exponent bytes 3 to 254 (4-bit mantissas) or 3 to 251 (8-bit) exactly, however many of them stand at its upper end; larger bytes are taken as that end.  The scaled query as in
  * kvbfp_decode_attention up to 32 heads.  A bias is as exact as fp32: relative to its own size (where every token that is seen is far away,
  * what they differ by).
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */

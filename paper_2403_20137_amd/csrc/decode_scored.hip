@@ -291,7 +291,8 @@ __device__ __forceinline__ void finish(const Args& a, int b, int kvh, int r0, in
 // Up to 16 rows: every wavefront has all of them and takes 32 tokens of a tile of 128 for itself.  With up to 8 rows (RP = 8) the 16
 // columns are these rows twice, once for either stage of 16 tokens: each lane then has four scores instead of eight, half of which would
 // be nobody's; the columns are joined in the end like another wavefront's (8 x 32768 tokens 68 us with them once, 64.5 twice).
-// grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL bf16 numbers of a query.
+// grid = (n_splits * B, H_kv); P mantissa bits, N16 blocks of 16, QL bf16 numbers of a query.  <8, true, 1, 16> and <8, true, 1, 8> spill 3 registers and 1
+// under three wavefronts a SIMD, which a workgroup needs 168 registers for; no other form does.
 template <int P, bool N16, int QL, int RP>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(QL == 1 ? 3 : 2))) void scored_split(Args a) {
     constexpr int PL = QL == 3 ? 3 : 2;
