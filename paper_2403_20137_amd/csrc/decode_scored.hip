@@ -11,10 +11,11 @@
 // A tile of 32 tokens whose tokens all precede the drafted ones and are seen by every row takes no mask; tiles that no row
 // sees (outside the window, the documents and the prefix) are not read.
 //
-// What bounds it.  Few rows and long sequences: 8 x 8 heads of 32768 tokens, four rows each, capped scores, 64 us (4.4 TB/s; the same
-// without the cap 62; 45 at the rate of a reading kernel): decoding to bf16 and the softmax take vector instructions about as long as the reading,
-// and three workgroups a compute unit overlap the two only in part.  Many rows: matrix and vector instructions, which hardly overlap within
-// a compute unit: 8 sequences of up to 8192 tokens with trees of 64 (256 rows a kv-head, capped) 150 us, 300 TFLOP/s of the two products; the second limb of the
+// What bounds it (times in a graph over three caches).  Few rows and long sequences: 8 x 8 heads of 32768 tokens, four rows each, capped scores, 61 us (4.7 TB/s; the
+// same without the cap 58; 45 at the rate of a reading kernel): decoding to bf16 and the softmax issue vector instructions in 69 % of the cycles,
+// and three workgroups a compute unit overlap them and the reading only in part.  Many rows: matrix and vector instructions, which hardly overlap within
+// a compute unit, as the wavefronts of a workgroup go in step: 8 sequences of up to 8192 tokens with trees of 64 (256 rows a kv-head, capped) 152 us,
+// 294 TFLOP/s of the two products, vector instructions in 72 % of the cycles, matrix instructions in 24 %; the second limb of the
 // probabilities is a third of the matrix work and stays, as one bf16 is off by 2^-9 of every weight.  A short sequence: the way of
 // the first loads and of the code itself, 7 to 9 us; loops that run once are not unrolled where that only makes them longer.
 // Measured and not kept: products of the next tile ahead of the values of this one, two tiles in flight, four workgroups a compute unit, 32 rows a

@@ -5,8 +5,9 @@
 // groups are added once at the end: no atomics, the same bits every time.  A wavefront has 32 tokens at a time as operands (the keys go
 // from memory to the operand, 32 channels a lane) and goes through up to 128 rows (fp32 I/O 64), which lie in LDS as operands; more rows are
 // further passes over the keys, which add to what the pass before has written.
-// 8 x 8 heads of 32768 tokens, four rows each: 35 us, 4.5 TB/s (25 for the reading alone, vector instructions 14).  Many rows are bound by the
-// exponentials, few tokens by the way of the code and of the first loads: one tile in flight with the loop once took 22.5 us for 4 x 265 rows of 78
+// 8 x 8 heads of 32768 tokens, four rows each: 34.7 us in a graph, 4.6 TB/s (25 for the reading alone, vector instructions 14).  Many rows and few tokens are bound
+// by the set-up: 128 rows of 3000 tokens turn into operands in every workgroup for three tiles (vector instructions 39 % of the time, bank conflicts
+// of the 2-byte stores 11 %, exponentials 3 %), and by the way of code and first loads: one tile in flight with the loop once took 22.5 us for 4 x 265 rows of 78
 // tokens where two with the loop twice took 26.9, and as long for long sequences.
 #include <hip/hip_runtime.h>
 
